@@ -58,7 +58,8 @@ enum kvm_status {
     KVM_E_UNSUPPORTED = -7, /* valid request this build cannot run (e.g. non-causal) */
     KVM_E_CUDA = -8,        /* the CUDA runtime refused a launch, a copy or a driver lookup */
     KVM_E_DEVICE_TIMEOUT = -9, /* only ever appears in kvm_stats.status: a bounded device wait gave up */
-    KVM_E_STATIC_LIMIT = -10 /* kvm_score_static: the problem does not fit the built-in scratch (see KVM_STATIC_SCORE_ROWS) */
+    KVM_E_STATIC_LIMIT = -10, /* kvm_score_static: the problem does not fit the built-in scratch (see KVM_STATIC_SCORE_ROWS) */
+    KVM_E_PAGE = -11         /* only ever appears in kvm_stats.status: a row's page number is outside the pool, or a unit has no page left for it */
 };
 
 /* The paper's problem statement as a plain struct (Section 2.4; hyper-parameters of Section 5.1). */
@@ -307,6 +308,101 @@ int kvm_prefill_attend(const kvm_params* p, const void* Q, const void* K, const 
  */
 int kvm_attend(const kvm_params* p, const void* q, const void* K, const void* V, int32_t rows, const int32_t* len,
                float* out, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Serving with compressed caches.  After the prefill a cache grows again: every decode step adds a row to each unit, and units
+ * hold different numbers of rows (kvm_compress's out_len).  A paged cache keeps the rows of a unit in pages of its own, so
+ * that a unit takes no more memory than its rows need:
+ *   K, V   device [n_pages, page_rows, D] in p->dtype, 16-byte aligned
+ *   table  device [U, max_pages] i32: the pages of each unit in order; entries past its rows are not read
+ *   len    device [U] i32: rows that each unit holds
+ *   page_rows  a power of two from 16 to 4096
+ * A row whose page number lies outside [0, n_pages) does not exist: it is neither written nor attended to, and
+ * kvm_stats.status says KVM_E_PAGE.  Lengths below 0 count as 0, above max_pages * page_rows as that.  A page that two units
+ * share is read by both; appending to it is the caller's mistake (the rows written last stay).
+ * Of kvm_params the functions below use the batch, heads, head_dim, dtype and softmax_scale only (seq, budget and the rules
+ * may be anything).  They keep nothing between calls and synchronise nothing: all of them can be captured into a CUDA graph,
+ * and since lengths and tables are read on the device a replayed graph follows them.
+ */
+typedef struct kvm_pages {
+    void *K, *V;
+    const int32_t* table;
+    const int32_t* len;
+    int32_t n_pages, page_rows, max_pages, reserved; /* reserved: 0 */
+} kvm_pages;
+
+enum kvm_rope_layout {
+    KVM_ROPE_HALVES = 0,     /* channel i is rotated with channel i + D/2 */
+    KVM_ROPE_NEIGHBOURS = 1  /* channel 2i is rotated with channel 2i + 1 */
+};
+#define KVM_MAX_ROWS (1 << 24) /* rows of a unit of a paged cache, or of a cache for kvm_shared_attend and kvm_cross_attend */
+
+/*
+ * The rotation's frequencies, as kvm_paged_append takes them: turns[i] = base^(-2i/head_dim) / (2 pi), the part of a full turn
+ * that pair i makes per position, as a 64-bit binary fraction (units of 2^-64 turns), for i < head_dim / 2.  Host only, and
+ * `turns` is HOST memory; the caller copies it to the device once.  A caller with other frequencies (scaled ones, say) fills
+ * the table itself.  The product of a position with such a number wraps around at whole turns by itself, so that
+ * angles of far positions lose nothing.  base: finite, > 1 (KVM_E_PARAM).
+ */
+int kvm_rope_turns(int32_t head_dim, double base, uint64_t* turns);
+
+/*
+ * Appends new tokens to a paged cache and rotates keys and queries by their positions on the way.
+ *   n_new    tokens per sequence, >= 1; token t of batch entry b stands at position pos[b] + t
+ *   new_len  NULL (every unit takes all n_new), or device [U] i32: how many of them each unit takes (clamped to 0..n_new)
+ *   pos      device [batch] i32, may be NULL when turns is
+ *   turns    device [D/2] u64, 8-byte aligned (kvm_rope_turns), or NULL: nothing is rotated, as for rows that are already
+ *            (a compressed cache moves into pages with k = K_out, v = V_out, n_new = cap, new_len = out_len)
+ *   rope_layout  kvm_rope_layout
+ *   q        NULL, or device [batch, n_q_heads, n_new, D];  k, v  device [batch, n_kv_heads, n_new, D], in p->dtype.  Their
+ *            strides may differ (q, k, v as they lie in a projection's output):
+ *   strides  NULL (contiguous), or a HOST array of 9: for q, k, v the strides of batch entry, head and token in elements,
+ *            each a multiple of 16 bytes and >= 0; channels are contiguous
+ *   q_out    device [batch, n_q_heads, n_new, D] contiguous (NULL when q is): the rotated queries of all n_new tokens; may be
+ *            q itself where q is contiguous, and may not overlap the inputs otherwise
+ *   c        the cache: row len[u] + t of unit u receives the rotated key and the value; other rows are left as they are
+ *   len_out  device [U] i32, written: the new lengths (at most max_pages * page_rows); c->len itself, or apart from it
+ * fp32 arithmetic, one rounding at the store; angles are exact to 2^-25 of a turn.  stats: NULL or a device kvm_stats.
+ */
+int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, int32_t n_new, const int32_t* new_len,
+                     const int32_t* pos, const uint64_t* turns, int32_t rope_layout, const void* q, const void* k,
+                     const void* v, const int64_t* strides, void* q_out, kvm_stats* stats, void* cuda_stream);
+
+/*
+ * One decode step of attention (Eq. 1) for a batch whose sequences share a prefix, such as a prompt that was prefilled and
+ * compressed once: the prefix is read once for all of them, not once per sequence.
+ *   q            [batch, n_q_heads, D] in p->dtype
+ *   K_pre, V_pre NULL (no prefix: decode attention over a paged cache), or [n_kv_heads, pre_rows, D] in p->dtype, as
+ *                kvm_compress leaves them for a batch of one; pre_rows <= KVM_MAX_ROWS
+ *   pre_len      NULL (every KV head holds pre_rows rows) or device [n_kv_heads] i32 (clamped to 0..pre_rows)
+ *   own          NULL (no rows beside the prefix), or the paged cache of the sequences' own rows; not written
+ *   out          [batch, n_q_heads, D] in p->dtype, written: softmax over the prefix's and the own rows together; zeros where there
+ *                are none; NaN where a bounded wait inside the kernel gave up
+ * bf16: fp32 accumulation and softmax, the weights enter the product with V rounded to bf16 and are divided by the sum of the
+ * rounded ones; fp32: fp32 arithmetic.  At least one of K_pre and own is given.
+ */
+int kvm_shared_workspace_bytes(const kvm_params* p, int32_t pre_rows, const kvm_pages* own, size_t* bytes);   /* Host only; pre_rows 0: no prefix. */
+int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, const void* V_pre, int32_t pre_rows,
+                      const int32_t* pre_len, const kvm_pages* own, void* out, kvm_stats* stats, void* ws, size_t ws_bytes,
+                      void* cuda_stream);
+
+/*
+ * Attention of n_q queries per head over a cache of another length: every query sees all the rows its unit holds (an
+ * encoder's states, a compressed cache; tokens drafted ahead of their verification as well as a whole chunk).
+ *   Q    [batch, n_q_heads, n_q, D];  K, V [batch, n_kv_heads, rows, D], in p->dtype; n_q <= KVM_MAX_SEQ, rows <= KVM_MAX_ROWS
+ *   len  NULL (every unit holds `rows` rows) or device [U] i32 (clamped to 0..rows); rows past it may hold anything
+ *   O_in, lse_in  NULL, or the attention of the same queries over other keys, O_in [batch, n_q_heads, n_q, D] in p->dtype and
+ *        lse_in [batch, n_q_heads, n_q] fp32, natural log: the result is then that over both sets of keys.  The next chunk of a
+ *        prompt attends to its compressed past and to itself by kvm_prefill_attend, whose O and lse go in here.  Both or neither;
+ *        they may be O and lse themselves, and may not overlap them otherwise
+ *   O    [batch, n_q_heads, n_q, D] in p->dtype, written; a unit with no rows gives zeros (or O_in)
+ *   lse  [batch, n_q_heads, n_q] fp32, written: ln of the sum over the keys of exp(scale * q.k); -inf without keys (or lse_in)
+ * Numerics as kvm_shared_attend.  bf16: a bounded wait that gave up leaves NaN and kvm_stats.status = KVM_E_DEVICE_TIMEOUT.
+ */
+int kvm_cross_workspace_bytes(const kvm_params* p, int32_t n_q, int32_t rows, size_t* bytes);   /* Host only. */
+int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void* K, const void* V, int32_t rows,
+                     const int32_t* len, const void* O_in, const float* lse_in, void* O, float* lse, kvm_stats* stats, void* ws,
+                     size_t ws_bytes, void* cuda_stream);
 
 /*
  * The criterion of Definition 2.1 for one decode step: attention outputs over the full cache (K, V

@@ -26,9 +26,12 @@ EXPORTS = (
     "kvm_sizes", "kvm_workspace_bytes", "kvm_score", "kvm_row_lse", "kvm_segment", "kvm_merge_compact", "kvm_compress",
     "kvm_compress_with_lse", "kvm_compress_layers", "kvm_compress_layers_filled", "kvm_layers_workspace_bytes",
     "kvm_host_staging_bytes", "kvm_compress_host", "kvm_score_static", "kvm_layer_ratio", "kvm_attend",
-    "kvm_output_perturbation", "kvm_prefill_attend", "kvm_status_string",
+    "kvm_output_perturbation", "kvm_prefill_attend", "kvm_rope_turns", "kvm_paged_append", "kvm_shared_workspace_bytes",
+    "kvm_shared_attend", "kvm_cross_workspace_bytes", "kvm_cross_attend", "kvm_status_string",
     "kvm_version",
 )
+KVM_ROPE_HALVES, KVM_ROPE_NEIGHBOURS = 0, 1
+KVM_E_PAGE = -11
 KVM_STATIC_SCORE_ROWS = 1 << 20
 
 
@@ -54,6 +57,15 @@ class KvmStats(ctypes.Structure):
     ]
 
 
+class KvmPages(ctypes.Structure):
+    """Mirror of `kvm_pages`.  `make_pages` fills it and keeps the tensors alive."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 class KvmError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -65,6 +77,7 @@ _F = {}          # entry points of the loaded library, argument types declared
 
 _P, _I, _Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
 _PARAMS = ctypes.POINTER(KvmParams)
+_PAGES = ctypes.POINTER(KvmPages)
 # Argument types as in include/kvm.h: with them declared, pointers pass as plain integers (a ctypes object per argument
 # costs more than the call).
 _ARGTYPES = {
@@ -86,6 +99,12 @@ _ARGTYPES = {
     "kvm_compress_layers_filled": (_PARAMS, _I) + (_P,) * 10 + (_Z, _P),
     "kvm_layers_workspace_bytes": (_PARAMS, _I, ctypes.POINTER(_Z)),
     "kvm_compress_host": (_PARAMS,) + (_P,) * 8 + (_Z, _P),
+    "kvm_rope_turns": (_I, ctypes.c_double, _P),
+    "kvm_paged_append": (_PARAMS, _PAGES, _P, _I, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P),
+    "kvm_shared_workspace_bytes": (_PARAMS, _I, _PAGES, ctypes.POINTER(_Z)),
+    "kvm_shared_attend": (_PARAMS, _P, _P, _P, _I, _P, _PAGES, _P, _P, _P, _Z, _P),
+    "kvm_cross_workspace_bytes": (_PARAMS, _I, _I, ctypes.POINTER(_Z)),
+    "kvm_cross_attend": (_PARAMS, _P, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _Z, _P),
 }
 
 
@@ -249,6 +268,117 @@ def kvm_compress_host(p: KvmParams, Q, K, V, K_out, V_out, out_len, out_pos, dev
     """Q..out_pos are HOST tensors (pin them for asynchronous copies); `dev` is a device byte buffer."""
     _call("kvm_compress_host", p, _ptr(Q), _ptr(K), _ptr(V), _ptr(K_out), _ptr(V_out), _ptr(out_len), _ptr(out_pos),
           _ptr(dev), dev.nbytes, _stream(stream))
+
+
+# ----------------------------------------------------------------------------- serving with compressed caches
+_TORCH_DTYPE = {KVM_BF16: torch.bfloat16, KVM_F32: torch.float32}
+
+
+def _arg(t: Optional[torch.Tensor], dtype, shape, name: str, strided: bool = False) -> Optional[int]:
+    """Address of a CUDA tensor of the current device, of this type and shape (the kernels take sizes from the parameters,
+    so a tensor of another shape would be read past its end)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda or t.get_device() != _device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device, got {t.device}")
+    if not strided and not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    return t.data_ptr()
+
+
+def _lengths(t: Optional[torch.Tensor], units: int, name: str) -> Optional[int]:
+    """int32 lengths, one per unit, in any shape of as many elements."""
+    return None if t is None else _arg(t.reshape(-1) if t.is_contiguous() else t, torch.int32, (units,), name)
+
+
+def rope_turns(head_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The rotation's frequencies as kvm_paged_append takes them (kvm_rope_turns): int64 [head_dim / 2] on `device`."""
+    host = torch.empty(max(1, head_dim // 2), dtype=torch.int64)
+    lib()
+    rc = _F["kvm_rope_turns"](head_dim, base, host.data_ptr())
+    if rc != KVM_OK:
+        raise KvmError(rc, "kvm_rope_turns")
+    return host.to(device)
+
+
+def make_pages(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: torch.Tensor) -> KvmPages:
+    """A paged cache: pools K, V [n_pages, page_rows, D], page numbers [units, max_pages] (or [batch, n_kv_heads, max_pages])
+    and lengths of the units, int32.  It holds on to the tensors, whose contents may change between calls."""
+    if K.dim() != 3 or not K.is_cuda or table.dim() < 2 or K.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("expected pools [n_pages, page_rows, head_dim] and page numbers [units, max_pages] on a CUDA device")
+    c = KvmPages(_arg(K, K.dtype, K.shape, "K"), _arg(V, K.dtype, K.shape, "V"), _arg(table, torch.int32, table.shape, "table"),
+                 _lengths(length, table.numel() // max(1, table.shape[-1]), "length"), K.shape[0], K.shape[1], table.shape[-1], 0)
+    c.tensors = (K, V, table, length)
+    return c
+
+
+def _check_pages(p: KvmParams, c: KvmPages) -> None:
+    K, _, table, _ = c.tensors
+    units = p.batch * p.n_kv_heads
+    if K.shape[2] != p.head_dim or K.dtype is not _TORCH_DTYPE.get(p.dtype) or table.numel() != units * c.max_pages:
+        raise ValueError(f"the cache is {K.dtype}, {table.numel() // c.max_pages} units of {K.shape[2]} channels; "
+                         f"the parameters say {units} of {p.head_dim}")
+
+
+def kvm_paged_append(p: KvmParams, cache: KvmPages, pos, turns, q, k, v, q_out, len_out, new_len=None, interleaved: bool = False,
+                     stats=None, stream=None) -> None:
+    """New tokens behind a paged cache's rows, keys and queries rotated on the way.  q [batch, n_q_heads, n_new, D] (or None) and
+    k, v [batch, n_kv_heads, n_new, D] may be strided views whose channels are contiguous."""
+    _check_pages(p, cache)
+    B, Hq, Hkv, D, n, dt = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, k.shape[2], _TORCH_DTYPE[p.dtype]
+    strides = []
+    for t, heads, name in ((q, Hq, "q"), (k, Hkv, "k"), (v, Hkv, "v")):
+        if t is not None:
+            _arg(t, dt, (B, heads, n, D), name, strided=True)
+            if t.stride(3) != 1:
+                raise ValueError(f"{name}: channels must be contiguous")
+            strides += [0 if size == 1 else step for size, step in zip(t.shape[:3], t.stride())]
+        else:
+            strides += (0, 0, 0)
+    _call("kvm_paged_append", p, cache, _lengths(len_out, B * Hkv, "len_out"), n, _lengths(new_len, B * Hkv, "new_len"),
+          _arg(pos, torch.int32, (B,), "pos"), _arg(turns, torch.int64, (D // 2,), "turns"),
+          KVM_ROPE_NEIGHBOURS if interleaved else KVM_ROPE_HALVES, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          (ctypes.c_int64 * 9)(*strides), _arg(q_out, dt, (B, Hq, n, D), "q_out"), _ptr(stats), _stream(stream))
+
+
+def kvm_shared_workspace_bytes(p: KvmParams, pre_rows: int, own: Optional[KvmPages]) -> int:
+    n = ctypes.c_size_t()
+    _call("kvm_shared_workspace_bytes", p, pre_rows, own, n)
+    return n.value
+
+
+def kvm_shared_attend(p: KvmParams, q, K_pre, V_pre, pre_len, own: Optional[KvmPages], out, ws, stats=None, stream=None) -> None:
+    """One decode step over a shared prefix K_pre, V_pre [n_kv_heads, rows, D] (or [1, n_kv_heads, rows, D], as kvm_compress
+    leaves it for a batch of one; None: no prefix) and the rows of each sequence's own in pages (None: none)."""
+    B, Hq, Hkv, D, dt = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype]
+    rows = 0
+    if K_pre is not None:
+        rows = K_pre.shape[-2]
+        shape = (Hkv, rows, D) if K_pre.dim() == 3 else (1, Hkv, rows, D)
+        _arg(K_pre, dt, shape, "K_pre")
+        _arg(V_pre, dt, shape, "V_pre")
+    if own is not None:
+        _check_pages(p, own)
+    _call("kvm_shared_attend", p, _arg(q, dt, (B, Hq, D), "q"), _ptr(K_pre), _ptr(V_pre), rows, _lengths(pre_len, Hkv, "pre_len"),
+          own, _arg(out, dt, (B, Hq, D), "out"), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
+
+
+def kvm_cross_workspace_bytes(p: KvmParams, n_q: int, rows: int) -> int:
+    n = ctypes.c_size_t()
+    _call("kvm_cross_workspace_bytes", p, n_q, rows, n)
+    return n.value
+
+
+def kvm_cross_attend(p: KvmParams, Q, K, V, length, O, lse, ws, O_in=None, lse_in=None, stats=None, stream=None) -> None:
+    """Attention of Q [batch, n_q_heads, n_q, D] over K, V [batch, n_kv_heads, rows, D] (rows past `length` left out), joined with
+    O_in, lse_in if given: O like Q, and the natural-log log-sum-exp [batch, n_q_heads, n_q]."""
+    B, Hq, Hkv, D, dt, n, rows = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype], Q.shape[2], K.shape[2]
+    _call("kvm_cross_attend", p, _arg(Q, dt, (B, Hq, n, D), "Q"), n, _arg(K, dt, (B, Hkv, rows, D), "K"),
+          _arg(V, dt, (B, Hkv, rows, D), "V"), rows, _lengths(length, B * Hkv, "length"), _arg(O_in, dt, (B, Hq, n, D), "O_in"),
+          _arg(lse_in, torch.float32, (B, Hq, n), "lse_in"), _arg(O, dt, (B, Hq, n, D), "O"),
+          _arg(lse, torch.float32, (B, Hq, n), "lse"), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
 
 
 # ----------------------------------------------------------------------------- convenience

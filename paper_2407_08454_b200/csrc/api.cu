@@ -181,6 +181,7 @@ const char* kvm_status_string(int s) {
         case KVM_E_UNSUPPORTED: return "unsupported request";
         case KVM_E_CUDA: return "CUDA runtime error";
         case KVM_E_DEVICE_TIMEOUT: return "a bounded device-side wait gave up";
+        case KVM_E_PAGE: return "a page number outside the pool, or no page left for a row";
         case KVM_E_STATIC_LIMIT:
             return "batch * n_q_heads * seq exceeds the built-in scratch of kvm_score_static (KVM_STATIC_SCORE_ROWS rows in fp32, an eighth of that in bf16)";
         default: return "unknown status";

@@ -1,0 +1,118 @@
+// Joins the states that pieces of a softmax have left, two sets of them if need be (a shared prefix and a sequence's own rows),
+// into the rows of the output:  M = max m,  O = sum o 2^(m - M) / sum lr 2^(m - M),  lse = ln sum l 2^(m - M) + M ln 2.
+// A warp per row; pieces are taken in order, four at a time so that their loads leave together: results are reproducible.
+#include "serve.cuh"
+
+namespace kvm {
+namespace serve {
+namespace {
+
+constexpr int JOIN_NT = 128;
+
+template <int E> struct Sum {                   // E channels of a row
+    float m = -INFINITY, l = 0.f, lr = 0.f, o[E] = {};
+};
+
+template <int D, int E>
+__device__ __forceinline__ void add_pieces(Sum<E>& s, const States& st, long long first, long long second, int count, int row) {
+    constexpr int BATCH = 4;
+    const int lane = threadIdx.x & 31;
+    for (int i0 = 0; i0 < count; i0 += BATCH) {
+        float4 z[BATCH];
+        float x[BATCH][E], mn = s.m;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const bool in = i0 + i < count;
+            const long long slot = i0 + i == 0 ? first : second + (long long)(i0 + i - 1) * st.stride;
+            const long long r = (in ? slot : first) * st.rows + row;
+            z[i] = __ldcg(st.ml + r);
+            if (E == 4) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(st.o + r * D) + lane);
+                x[i][0] = v.x; x[i][1] = v.y; x[i][E - 2] = v.z; x[i][E - 1] = v.w;
+            } else {
+                const float2 v = __ldcg(reinterpret_cast<const float2*>(st.o + r * D) + lane);
+                x[i][0] = v.x; x[i][1] = v.y;
+            }
+            if (!in) z[i].x = -INFINITY;
+            mn = fmaxf(mn, z[i].x);
+        }
+        const float a = rescale2(s.m, mn);
+        s.l *= a; s.lr *= a;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s.o[e] *= a;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i0 + i >= count) break;
+            // (an empty state weighs nothing; a state that gave up is NaN whatever its reference says)
+            const float w = z[i].y == 0.f ? 0.f : rescale2(z[i].x, mn);
+            s.l = fmaf(z[i].y, w, s.l);
+            s.lr = fmaf(z[i].z, w, s.lr);
+            if (w != 0.f)
+#pragma unroll
+                for (int e = 0; e < E; ++e) s.o[e] = fmaf(x[i][e], w, s.o[e]);
+        }
+        s.m = mn;
+    }
+}
+
+// len: of the units of `a` whose pieces the table tells of (a unit without keys has no entry there).
+template <typename T, int D>
+__global__ void __launch_bounds__(JOIN_NT) join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, int has_a, int has_b,
+                                                       const int32_t* __restrict__ b_len, int skip_whole, const Output out, long long rows, int m_rows,
+                                                       int Hkv, int G) {
+    constexpr int E = D / 32;
+    const int lane = threadIdx.x & 31;
+    const long long w = (long long)blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    if (w >= rows) return;
+    const int u = (int)(w / m_rows), m = (int)(w % m_rows);
+    Sum<E> s;
+    auto add = [&](const States& st, const int32_t* len, int unit, int row_of_unit) {       // false: written by its kernel
+        int item, row;
+        st.find(row_of_unit, item, row);
+        const long long at = (long long)unit * st.items + item;
+        if (st.count > 0) {
+            add_pieces<D, E>(s, st, at * st.count, at * st.count + 1, st.count, row);
+        } else if (!len || __ldg(len + unit) > 0) {
+            const int4 pc = __ldcg(st.pieces + at);
+            if (skip_whole && pc.x == 1) return false;
+            add_pieces<D, E>(s, st, pc.y, pc.z, pc.x, row);
+        }
+        return true;
+    };
+    if (has_b && !add(b, b_len, u % Hkv, u / Hkv * G + m)) return;
+    if (has_a && !add(a, a_len, u, m)) return;
+    const RowEnd end(s.m, s.l, s.lr, out.lse_in, w);
+    float y[E], x[E] = {};
+    T* orow = (T*)out.O + w * D + lane * E;
+    if (out.O_in) {
+        const T* irow = (const T*)out.O_in + w * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = (float)irow[e];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = end_value(s.o[e], end.f, x[e], end.f_in);
+    if (sizeof(T) == 2) {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) reinterpret_cast<uint32_t*>(orow)[e / 2] = Vec<__nv_bfloat16>::pack2(y[e], y[e + 1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) orow[e] = (T)y[e];
+    }
+    if (out.lse && lane == 0) out.lse[w] = end.lse;
+}
+
+}  // namespace
+
+cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
+                        int skip_whole, const Output& out, cudaStream_t st) {
+    const long long rows = (long long)units * m, blocks = (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>)
+                                  : (s.D == 128 ? join_kernel<float, 128> : join_kernel<float, 64>);
+    return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, a_len, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
+                            b_len, skip_whole, out, rows, m, s.Hkv, s.G);
+}
+
+}  // namespace serve
+}  // namespace kvm

@@ -1,0 +1,138 @@
+// What the serving kernels share (paged append, shared-prefix decode, cross attention): where query and key rows lie, the
+// states that parts of a softmax leave, and how they are joined.
+#pragma once
+#include "common.cuh"
+
+namespace kvm {
+namespace serve {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// The shape part of kvm_params, checked.
+struct Shape {
+    int B, Hq, Hkv, G, D, U, dtype;
+    float scale;
+};
+
+// A paged cache as the kernels take it.
+struct Pages {
+    void *K, *V;
+    const int32_t *table, *len;
+    int n_pages, shift, max_pages;              // rows per page: 1 << shift
+    __host__ __device__ __forceinline__ int room() const { return max_pages << shift; }
+};
+
+// Query rows of a unit: N blocks of R rows of D channels; unit u's block n starts at row u * su + n * sn of the tensor.  Outputs
+// lie alike.
+//   cross attention: unit = (b, h), its G heads' n_q rows follow one another: R = G n_q, N = 1
+//   a shared prefix: unit = h, block = b: R = G, N = B;  a sequence's own rows: unit = (b, h), R = G, N = 1
+struct Queries {
+    const void* q;
+    long long su, sn;
+    int R, N;
+    __host__ __device__ __forceinline__ int rows() const { return R * N; }
+    __device__ __forceinline__ long long at(int u, int m) const { return u * su + (m / R) * sn + m % R; }
+};
+
+// Key rows of a unit: contiguous (K, V [units, rows, D]) or paged.
+struct Keys {
+    const void *K, *V;
+    const int32_t* len;                         // nullable: all `rows`
+    int rows;                                   // most rows of a unit
+    const int32_t* table;                       // nullable: contiguous
+    int n_pages, shift, max_pages;
+    __device__ __forceinline__ int rows_of(int u) const { return len ? max(0, min(__ldg(len + u), rows)) : rows; }
+    // index of a unit's row in the tensor of all rows, or -1 where its page does not exist
+    __device__ __forceinline__ long long row(int u, int r) const {
+        if (!table) return (long long)u * rows + r;
+        const int page = __ldg(table + (size_t)u * max_pages + (r >> shift));
+        return (unsigned)page < (unsigned)n_pages ? ((long long)page << shift) + (r & ((1 << shift) - 1)) : -1;
+    }
+};
+
+// The states of pieces of a softmax.  A piece covers the query rows of an item (a tile of a unit's query rows, or two) over some of
+// the unit's keys; its state, in a slot of its own, is per row the weighted sum of the values o[D] and (m, l, lr): the reference
+// (log2 units), the sum of the weights relative to it, and the sum of the weights as they were rounded for the product.
+struct States {
+    float* o;                                   // [slot][rows][D]
+    float4* ml;                                 // [slot][rows]
+    int rows;                                   // rows of a slot
+    int items;                                  // items of a unit
+    int count;                                  // pieces of every item, in slots item * count ..; 0: `pieces` tells
+    int4* pieces;                               // per item (count, first slot, second slot, -); the others follow the second by `stride`
+    int stride;
+    // Which rows an item holds.  Tiles of `tile` consecutive rows of a unit; or (R > 0) each block of R rows in tiles of its own.
+    int tile, R, two;                           // two: two tiles to an item, `tile_room` rows apart
+    int tile_room;
+    __device__ __forceinline__ void find(int m, int& item, int& row) const {
+        int t, in;
+        if (R > 0) {
+            const int n = m / R, r = m % R;
+            t = n * ((R + tile - 1) / tile) + r / tile;
+            in = r % tile;
+        } else {
+            t = m / tile;
+            in = m % tile;
+        }
+        item = two ? t >> 1 : t;
+        row = two ? (t & 1) * tile_room + in : in;
+    }
+};
+// Where the result goes, and what is joined in.
+struct Output {
+    void* O;
+    float* lse;                                 // nullable
+    const void* O_in;                           // nullable
+    const float* lse_in;
+};
+
+inline size_t state_bytes(size_t slots, int rows, int D) { return slots * rows * ((size_t)D * 4 + sizeof(float4)); }
+
+// Weight of a state with reference m under the reference M (an empty state has m = -inf).
+__device__ __forceinline__ float rescale2(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
+
+// One row's result from its sums, N channels at a time: o / lr, joined with O_in under both log-sum-exps.
+// (l = 0: no keys.  NaN sums stay NaN.)
+struct RowEnd {
+    float f, f_in, lse;
+    __device__ __forceinline__ RowEnd(float m, float l, float lr, const float* lse_in, long long row) {
+        const bool none = l == 0.f;
+        f = none ? 0.f : 1.f / lr;
+        f_in = 0.f;
+        lse = none ? -INFINITY : (m + log2f(l)) * LN2;
+        if (lse_in) {
+            const float z = lse_in[row], M = fmaxf(lse, z);
+            if (M == -INFINITY) { lse = M; return; }             // neither has keys
+            const float a = expf(lse - M), b = expf(z - M), s = a + b;
+            f *= a / s;
+            f_in = b / s;
+            lse = M + logf(s);
+        }
+    }
+};
+// o * f + O_in * f_in; what has no weight counts as nothing, whatever it holds.
+__device__ __forceinline__ float end_value(float o, float f, float x, float f_in) {
+    const float y = f != 0.f ? o * f : 0.f;
+    return f_in != 0.f ? fmaf(x, f_in, y) : y;
+}
+
+cudaError_t launch_append(const Shape& s, const Pages& c, int32_t* len_out, int n_new, const int32_t* new_len, const int32_t* pos,
+                          const uint64_t* turns, int neighbours, const void* q, const void* k, const void* v, const int64_t* strides,
+                          void* q_out, kvm_stats* stats, cudaStream_t st);
+
+// Attention of all query rows over all keys of their units, by fp32 arithmetic on the ordinary cores.  With one piece per item the
+// result goes to `out`, else the states to `states`.
+struct SimtPlan {
+    int mt, items, pieces;                      // query rows of an item, items of a unit, pieces of an item
+};
+SimtPlan simt_plan(int units, int m, int rows);
+cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
+                             kvm_stats* stats, cudaStream_t st);
+
+// Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
+// unit = h and row = b * G + g, of `b` (a shared prefix).
+cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len, int skip_whole,
+                        const Output& out, cudaStream_t st);
+
+}  // namespace serve
+}  // namespace kvm

@@ -1,0 +1,114 @@
+"""kvm_cross_attend against 64 bits: output and log-sum-exp, ragged and empty units, joined with other keys' attention."""
+import math
+
+import pytest
+import torch
+
+import paper_2407_08454_b200 as kvm
+from serve_ref import Rows, close
+
+pytestmark = pytest.mark.gpu
+
+
+def check(B, Hq, Hkv, n_q, rows, D, dtype, join=False, lengths="ragged", in_place=False, seed=0, scale=0.0):
+    g = torch.Generator().manual_seed(seed + B + Hq * 3 + n_q * 5 + rows)
+    G, U = Hq // Hkv, B * Hkv
+    p = kvm.make_params(B, Hq, Hkv, 1, D, dtype, softmax_scale=scale)
+    Q = (2.0 * torch.randn(B, Hq, n_q, D, generator=g)).to(dtype)
+    K, V = (torch.randn(B, Hkv, rows, D, generator=g).to(dtype) for _ in range(2))
+    ln = torch.full((B, Hkv), rows, dtype=torch.int32)
+    if lengths == "ragged":
+        ln = torch.randint(0, rows + 1, (B, Hkv), generator=g, dtype=torch.int32)
+        ln.view(-1)[-1] = rows
+        if U > 1:
+            ln.view(-1)[0] = 0
+    for u in range(U):
+        K.view(U, rows, D)[u, int(ln.view(-1)[u]):] = math.nan
+        V.view(U, rows, D)[u, int(ln.view(-1)[u]):] = math.inf
+    O_in = lse_in = None
+    if join:
+        O_in = torch.randn(B, Hq, n_q, D, generator=g).to(dtype)
+        lse_in = 3.0 * torch.randn(B, Hq, n_q, generator=g) + math.log(max(rows, 2))
+        lse_in[..., 0] = -math.inf                         # a query that has seen no other keys: its O_in may be anything
+        O_in[:, :, 0] = math.nan
+        lse_in[..., -1] += 200.0                           # ... and one for which the rows here weigh nothing
+    O = torch.full((B, Hq, n_q, D), math.nan, dtype=dtype, device="cuda")
+    lse = torch.full((B, Hq, n_q), math.nan, device="cuda")
+    a = b = None
+    if join:
+        a, b = O_in.cuda(), lse_in.cuda()
+        if in_place:
+            O, lse = a, b
+    ws = torch.full((kvm.kvm_cross_workspace_bytes(p, n_q, rows),), 255, dtype=torch.uint8, device="cuda")
+    stats = kvm.new_stats("cuda")
+    args = (p, Q.cuda(), K.cuda(), V.cuda(), None if lengths is None else ln.cuda())
+    kvm.kvm_cross_attend(*args, O, lse, ws, O_in=a, lse_in=b, stats=stats)
+    assert kvm.read_stats(stats).status == 0
+    if not in_place:
+        O2, lse2 = torch.empty_like(O), torch.empty_like(lse)
+        kvm.kvm_cross_attend(*args, O2, lse2, ws, O_in=a, lse_in=b)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    sc = scale if scale > 0 else 1.0 / math.sqrt(D)
+    for bi in range(B):
+        for h in range(Hq):
+            n = int(ln[bi, h // G])
+            ref = Rows(Q[bi, h], K[bi, h // G, :n], V[bi, h // G, :n], sc)
+            if join:
+                ref.joined(O_in[bi, h], lse_in[bi, h])
+            close(O[bi, h], ref.O, ref.O_bound(dtype), ("O", bi, h, n))
+            close(lse[bi, h], ref.lse, ref.lse_bound(), ("lse", bi, h, n))
+
+
+SHAPES = [
+    # B, Hq, Hkv, n_q, rows, D
+    (1, 1, 1, 1, 1, 128),
+    (2, 4, 2, 1, 300, 64),
+    (2, 4, 4, 1, 128, 128),
+    (3, 8, 2, 5, 1000, 128),              # drafted tokens
+    (1, 2, 2, 127, 129, 64),
+    (1, 2, 1, 128, 127, 128),             # 256 rows a head: two full tiles
+    (2, 6, 2, 43, 128, 128),              # 129 rows
+    (1, 3, 1, 200, 260, 64),              # 600: three tiles and a bit
+    (2, 2, 2, 300, 77, 128),
+    (1, 4, 1, 129, 513, 128),
+    (5, 5, 5, 64, 65, 64),
+    (1, 1, 1, 700, 1500, 128),
+    (8, 16, 8, 20, 200, 128),
+    (40, 8, 4, 3, 40, 64),                # more units than SMs
+    (1, 16, 16, 260, 390, 128),
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n_q,rows,D", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("join", [False, True])
+def test_cross_matches_64_bits(B, Hq, Hkv, n_q, rows, D, dtype, join):
+    check(B, Hq, Hkv, n_q, rows, D, dtype, join=join)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n_q", [3, 290])
+def test_cross_in_place_without_lengths_and_with_a_scale(dtype, n_q):
+    check(2, 8, 4, n_q, 333, 128, dtype, join=True, in_place=True)
+    check(2, 8, 4, n_q, 256, 64, dtype, lengths=None, scale=0.05)
+    check(1, 2, 2, n_q, 5000, 128, dtype, join=True)       # one unit's keys in many pieces
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_maximum_that_keeps_growing(dtype):
+    """Keys that outgrow one another by more than any step of a running reference, all through the sequence."""
+    B, H, n_q, rows, D = 1, 2, 140, 900, 128
+    g = torch.Generator().manual_seed(8)
+    u = torch.randn(H, 1, D, generator=g)
+    Q = (u / u.norm(dim=-1, keepdim=True) * torch.linspace(1.0, 8.0, n_q)[:, None]).to(dtype).view(B, H, n_q, D)
+    K = (u / u.norm(dim=-1, keepdim=True) * torch.linspace(-60.0, 120.0, rows)[:, None] + 0.1 * torch.randn(H, rows, D, generator=g)).to(dtype)
+    K = K.view(B, H, rows, D)
+    V = torch.randn(B, H, rows, D, generator=g).to(dtype)
+    p = kvm.make_params(B, H, H, 1, D, dtype)
+    O, lse = torch.empty(B, H, n_q, D, dtype=dtype, device="cuda"), torch.empty(B, H, n_q, device="cuda")
+    ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n_q, rows), dtype=torch.uint8, device="cuda")
+    kvm.kvm_cross_attend(p, Q.cuda(), K.cuda(), V.cuda(), None, O, lse, ws)
+    for h in range(H):
+        ref = Rows(Q[0, h], K[0, h], V[0, h], 1.0 / math.sqrt(D))
+        close(O[0, h], ref.O, ref.O_bound(dtype), h)
+        close(lse[0, h], ref.lse, ref.lse_bound(), h)

@@ -64,9 +64,26 @@ States simt_states(const SimtPlan& plan, int units, int D, Carver& c) {
     return s;
 }
 
+// States of the tensor-core kernel's pieces.
+States tc_states(const TcPlan& plan, int units, int D, int R, Carver& c) {
+    States s = {};
+    s.rows = plan.slot_rows;
+    s.items = plan.items;
+    s.stride = 2;
+    s.tile = plan.gx * plan.bx;
+    s.R = plan.per_block ? R : 0;
+    s.two = 1;
+    s.tile_room = 128;
+    s.o = (float*)c.take((size_t)plan.slots * plan.slot_rows * D * sizeof(float));
+    s.ml = (float4*)c.take((size_t)plan.slots * plan.slot_rows * sizeof(float4));
+    s.pieces = (int4*)c.take((size_t)units * plan.items * sizeof(int4));
+    return s;
+}
+
 // How a call of the decode attention is dealt, and what it needs of the workspace.
 struct SharedWork {
     bool pre, own;
+    TcPlan pre_tc;
     SimtPlan pre_plan, own_plan;
     States pre_states, own_states;
     size_t bytes;
@@ -76,7 +93,10 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
     Carver c{(char*)ws};
     w.pre = pre_rows > 0;
     w.own = own != nullptr;
-    if (w.pre) {
+    if (w.pre && s.dtype == KVM_BF16) {
+        w.pre_tc = tc_plan(s.Hkv, s.G, s.B, pre_rows, false);
+        w.pre_states = tc_states(w.pre_tc, s.Hkv, s.D, s.G, c);
+    } else if (w.pre) {
         w.pre_plan = simt_plan(s.Hkv, s.B * s.G, pre_rows);
         if (w.own || w.pre_plan.pieces > 1) w.pre_states = simt_states(w.pre_plan, s.Hkv, s.D, c);
     }
@@ -89,6 +109,7 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
 }
 
 struct CrossWork {
+    TcPlan tc;
     SimtPlan plan;
     States states;
     size_t bytes;
@@ -96,6 +117,12 @@ struct CrossWork {
 CrossWork plan_cross(const Shape& s, int n_q, int rows, void* ws) {
     CrossWork w = {};
     Carver c{(char*)ws};
+    if (s.dtype == KVM_BF16) {
+        w.tc = tc_plan(s.U, s.G * n_q, 1, rows, true);
+        w.states = tc_states(w.tc, s.U, s.D, s.G * n_q, c);
+        w.bytes = c.off + 256;
+        return w;
+    }
     w.plan = simt_plan(s.U, s.G * n_q, rows);
     if (w.plan.pieces > 1) w.states = simt_states(w.plan, s.U, s.D, c);
     w.bytes = c.off + 256;
@@ -194,7 +221,9 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (w.pre) {
         const Queries qs = {q, s.G, s.Hq, s.G, s.B};
         const Keys ks = {K_pre, V_pre, pre_len, pre_rows, nullptr, 0, 0, 0};
-        if (launch_rows_simt(s, w.pre_plan, s.Hkv, qs, ks, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        const cudaError_t e = s.dtype == KVM_BF16 ? launch_rows_tc(s, w.pre_tc, s.Hkv, qs, ks, w.pre_states, o, stats, st)
+                                                  : launch_rows_simt(s, w.pre_plan, s.Hkv, qs, ks, w.pre_states, o, stats, st);
+        if (e != cudaSuccess) return KVM_E_CUDA;
     }
     if (w.own) {
         const Queries qs = {q, s.G, 0, s.G, 1};
@@ -202,7 +231,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
         if (launch_rows_simt(s, w.own_plan, s.U, qs, ks, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
     if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
-    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, nullptr, w.pre ? &w.pre_states : nullptr, nullptr, 0, o, st) == cudaSuccess
+    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, nullptr, w.pre ? &w.pre_states : nullptr, pre_len, 0, o, st) == cudaSuccess
                ? KVM_OK
                : KVM_E_CUDA;
 }
@@ -234,6 +263,10 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     const Queries qs = {Q, m, 0, m, 1};
     const Keys ks = {K, V, len, rows, nullptr, 0, 0, 0};
     const Output o = {O, lse, O_in, lse_in};
+    if (s.dtype == KVM_BF16) {
+        if (launch_rows_tc(s, w.tc, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        return launch_join(s, s.U, m, &w.states, len, nullptr, nullptr, 1, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
     return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;

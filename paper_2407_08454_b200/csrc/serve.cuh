@@ -129,6 +129,17 @@ SimtPlan simt_plan(int units, int m, int rows);
 cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                              kvm_stats* stats, cudaStream_t st);
 
+// The same on the tensor cores (bf16, contiguous keys): equal shares of all items' steps per CTA, see rows_tc.cu.
+struct TcPlan {
+    int gx, bx;                                 // rows of a query tile: bx blocks of gx rows
+    int per_block, tiles, items;                // tiles of a block of more than 128 rows (else 0), tiles and items (pairs of tiles) of a unit
+    int direct, grid, slot_rows;                // direct: an item in one piece goes to the output
+    long long slots;
+};
+TcPlan tc_plan(int units, int R, int N, int rows, bool direct);
+cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
+                           kvm_stats* stats, cudaStream_t st);
+
 // Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
 // unit = h and row = b * G + g, of `b` (a shared prefix).
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len, int skip_whole,

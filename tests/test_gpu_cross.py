@@ -76,6 +76,8 @@ SHAPES = [
     (8, 16, 8, 20, 200, 128),
     (40, 8, 4, 3, 40, 64),                # more units than SMs
     (1, 16, 16, 260, 390, 128),
+    (3, 8, 8, 300, 1000, 128),            # more steps than SMs: shares that hold whole items and parts
+    (6, 8, 4, 200, 700, 64),
 ]
 
 

@@ -81,6 +81,7 @@ SHAPES = [
     (5, 40, 2, 64, 260, 50, 16),           # blocks of twenty rows
     (2, 136, 1, 128, 150, 20, 16),         # a block of more than 128 rows
     (9, 3, 3, 128, 1000, 100, 64),
+    (20, 64, 16, 64, 2500, 10, 16),        # more steps over the prefix than SMs
 ]
 
 

@@ -51,7 +51,7 @@ struct Carver {
     }
 };
 
-// States of a fixed number of pieces per item.
+// States of a fixed number of pieces per item (plan.mt rows each).
 States simt_states(const SimtPlan& plan, int units, int D, Carver& c) {
     States s = {};
     const size_t slots = (size_t)units * plan.items * plan.pieces;
@@ -100,7 +100,12 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
         w.pre_plan = simt_plan(s.Hkv, s.B * s.G, pre_rows);
         if (w.own || w.pre_plan.pieces > 1) w.pre_states = simt_states(w.pre_plan, s.Hkv, s.D, c);
     }
-    if (w.own) {
+    if (w.own && s.dtype == KVM_BF16) {
+        w.own_plan.mt = s.G;
+        w.own_plan.items = 1;
+        w.own_plan.pieces = paged_pieces(s, own->room());
+        if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
+    } else if (w.own) {
         w.own_plan = simt_plan(s.U, s.G, own->room());
         if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
     }
@@ -228,10 +233,12 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (w.own) {
         const Queries qs = {q, s.G, 0, s.G, 1};
         const Keys ks = {pg.K, pg.V, pg.len, pg.room(), pg.table, pg.n_pages, pg.shift, pg.max_pages};
-        if (launch_rows_simt(s, w.own_plan, s.U, qs, ks, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        const cudaError_t e = s.dtype == KVM_BF16 ? launch_rows_paged(s, w.own_plan.pieces, q, ks, w.own_states, out, stats, st)
+                                                  : launch_rows_simt(s, w.own_plan, s.U, qs, ks, w.own_states, o, stats, st);
+        if (e != cudaSuccess) return KVM_E_CUDA;
     }
     if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
-    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, nullptr, w.pre ? &w.pre_states : nullptr, pre_len, 0, o, st) == cudaSuccess
+    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, nullptr, w.pre ? &w.pre_states : nullptr, pre_len, o, st) == cudaSuccess
                ? KVM_OK
                : KVM_E_CUDA;
 }
@@ -265,11 +272,11 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     const Output o = {O, lse, O_in, lse_in};
     if (s.dtype == KVM_BF16) {
         if (launch_rows_tc(s, w.tc, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
-        return launch_join(s, s.U, m, &w.states, len, nullptr, nullptr, 1, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+        return launch_join_items(s, s.U, m, w.states, len, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
-    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
 }
 
 }  // extern "C"

@@ -140,10 +140,17 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct);
 cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                            kvm_stats* stats, cudaStream_t st);
 
+// Decode attention over a paged cache (bf16), one query per sequence: rows_paged.cu.
+int paged_pieces(const Shape& s, int rows);
+cudaError_t launch_rows_paged(const Shape& s, int pieces, const void* q, const Keys& k, const States& states, void* out, kvm_stats* stats,
+                              cudaStream_t st);
+
 // Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
 // unit = h and row = b * G + g, of `b` (a shared prefix).
-cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len, int skip_whole,
+cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
                         const Output& out, cudaStream_t st);
+// The same for the tensor-core kernel's items [units][items] of m rows a unit, of which those in one piece are in the output already.
+cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st);
 
 }  // namespace serve
 }  // namespace kvm

@@ -272,25 +272,40 @@ def kvm_compress_host(p: KvmParams, Q, K, V, K_out, V_out, out_len, out_pos, dev
 
 # ----------------------------------------------------------------------------- serving with compressed caches
 _TORCH_DTYPE = {KVM_BF16: torch.bfloat16, KVM_F32: torch.float32}
+_STRIDES = ctypes.c_int64 * 9
 
 
-def _arg(t: Optional[torch.Tensor], dtype, shape, name: str, strided: bool = False) -> Optional[int]:
-    """Address of a CUDA tensor of the current device, of this type and shape (the kernels take sizes from the parameters,
-    so a tensor of another shape would be read past its end)."""
+def _refuse(t: torch.Tensor, dtype, shape, name: str, strided: bool = False):
+    want = f"{tuple(shape)}" if isinstance(shape, tuple) else f"{shape} elements"
+    raise ValueError(f"{name}: expected a {'strided' if strided else 'contiguous'} {dtype} tensor of {want} on the current CUDA device, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _on(t: torch.Tensor) -> int:
+    """The current device, which has to be the tensor's."""
+    dev = t.get_device()
+    if dev < 0 or dev != _device():
+        raise ValueError(f"expected tensors on the current CUDA device, got one on {t.device}")
+    return dev
+
+
+def _arg(t: Optional[torch.Tensor], dtype, shape, name: str, dev: int) -> Optional[int]:
+    """Address of a contiguous CUDA tensor of the current device, of this type and shape (the kernels take sizes from the
+    parameters, so a tensor of another shape would be read past its end)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if not t.is_cuda or t.get_device() != _device():
-        raise ValueError(f"{name}: expected a tensor on the current CUDA device, got {t.device}")
-    if not strided and not t.is_contiguous():
-        raise ValueError(f"{name}: must be contiguous")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, dtype, shape, name)
     return t.data_ptr()
 
 
-def _lengths(t: Optional[torch.Tensor], units: int, name: str) -> Optional[int]:
+def _lengths(t: Optional[torch.Tensor], units: int, name: str, dev: int) -> Optional[int]:
     """int32 lengths, one per unit, in any shape of as many elements."""
-    return None if t is None else _arg(t.reshape(-1) if t.is_contiguous() else t, torch.int32, (units,), name)
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() != units or t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, torch.int32, units, name)
+    return t.data_ptr()
 
 
 def rope_turns(head_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -308,39 +323,37 @@ def make_pages(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, length: to
     and lengths of the units, int32.  It holds on to the tensors, whose contents may change between calls."""
     if K.dim() != 3 or not K.is_cuda or table.dim() < 2 or K.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("expected pools [n_pages, page_rows, head_dim] and page numbers [units, max_pages] on a CUDA device")
-    c = KvmPages(_arg(K, K.dtype, K.shape, "K"), _arg(V, K.dtype, K.shape, "V"), _arg(table, torch.int32, table.shape, "table"),
-                 _lengths(length, table.numel() // max(1, table.shape[-1]), "length"), K.shape[0], K.shape[1], table.shape[-1], 0)
-    c.tensors = (K, V, table, length)
+    dev, units = K.get_device(), table.numel() // max(1, table.shape[-1])
+    c = KvmPages(_arg(K, K.dtype, K.shape, "K", dev), _arg(V, K.dtype, K.shape, "V", dev), _arg(table, torch.int32, table.shape, "table", dev),
+                 _lengths(length, units, "length", dev), K.shape[0], K.shape[1], table.shape[-1], 0)
+    c.tensors, c.of = (K, V, table, length), (dev, units, K.shape[2], K.dtype)
     return c
 
 
-def _check_pages(p: KvmParams, c: KvmPages) -> None:
-    K, _, table, _ = c.tensors
-    units = p.batch * p.n_kv_heads
-    if K.shape[2] != p.head_dim or K.dtype is not _TORCH_DTYPE.get(p.dtype) or table.numel() != units * c.max_pages:
-        raise ValueError(f"the cache is {K.dtype}, {table.numel() // c.max_pages} units of {K.shape[2]} channels; "
-                         f"the parameters say {units} of {p.head_dim}")
+def _check_pages(c: KvmPages, dev: int, units: int, head_dim: int, dtype) -> None:
+    if c.of != (dev, units, head_dim, dtype):
+        raise ValueError(f"the cache is of (device, units, channels, type) {c.of}; the call is for {(dev, units, head_dim, dtype)}")
 
 
 def kvm_paged_append(p: KvmParams, cache: KvmPages, pos, turns, q, k, v, q_out, len_out, new_len=None, interleaved: bool = False,
                      stats=None, stream=None) -> None:
     """New tokens behind a paged cache's rows, keys and queries rotated on the way.  q [batch, n_q_heads, n_new, D] (or None) and
     k, v [batch, n_kv_heads, n_new, D] may be strided views whose channels are contiguous."""
-    _check_pages(p, cache)
-    B, Hq, Hkv, D, n, dt = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, k.shape[2], _TORCH_DTYPE[p.dtype]
-    strides = []
-    for t, heads, name in ((q, Hq, "q"), (k, Hkv, "k"), (v, Hkv, "v")):
-        if t is not None:
-            _arg(t, dt, (B, heads, n, D), name, strided=True)
-            if t.stride(3) != 1:
-                raise ValueError(f"{name}: channels must be contiguous")
-            strides += [0 if size == 1 else step for size, step in zip(t.shape[:3], t.stride())]
-        else:
+    B, Hq, Hkv, D, n, dt, dev = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, k.shape[2], _TORCH_DTYPE[p.dtype], _on(k)
+    units, kv, strides = B * Hkv, (B, Hkv, n, D), []
+    _check_pages(cache, dev, units, D, dt)
+    for t, shape, name in ((q, (B, Hq, n, D), "q"), (k, kv, "k"), (v, kv, "v")):
+        if t is None:
             strides += (0, 0, 0)
-    _call("kvm_paged_append", p, cache, _lengths(len_out, B * Hkv, "len_out"), n, _lengths(new_len, B * Hkv, "new_len"),
-          _arg(pos, torch.int32, (B,), "pos"), _arg(turns, torch.int64, (D // 2,), "turns"),
+            continue
+        sb, sh, st, sd = t.stride()
+        if t.dtype is not dt or t.shape != shape or t.get_device() != dev or sd != 1:
+            _refuse(t, dt, shape, name, strided=True)
+        strides += (sb if B > 1 else 0, sh if shape[1] > 1 else 0, st if n > 1 else 0)     # (of one: whatever the view says)
+    _call("kvm_paged_append", p, cache, _lengths(len_out, units, "len_out", dev), n, _lengths(new_len, units, "new_len", dev),
+          _arg(pos, torch.int32, (B,), "pos", dev), _arg(turns, torch.int64, (D // 2,), "turns", dev),
           KVM_ROPE_NEIGHBOURS if interleaved else KVM_ROPE_HALVES, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
-          (ctypes.c_int64 * 9)(*strides), _arg(q_out, dt, (B, Hq, n, D), "q_out"), _ptr(stats), _stream(stream))
+          _STRIDES(*strides), _arg(q_out, dt, (B, Hq, n, D), "q_out", dev), _ptr(stats), _stream(stream))
 
 
 def kvm_shared_workspace_bytes(p: KvmParams, pre_rows: int, own: Optional[KvmPages]) -> int:
@@ -352,17 +365,18 @@ def kvm_shared_workspace_bytes(p: KvmParams, pre_rows: int, own: Optional[KvmPag
 def kvm_shared_attend(p: KvmParams, q, K_pre, V_pre, pre_len, own: Optional[KvmPages], out, ws, stats=None, stream=None) -> None:
     """One decode step over a shared prefix K_pre, V_pre [n_kv_heads, rows, D] (or [1, n_kv_heads, rows, D], as kvm_compress
     leaves it for a batch of one; None: no prefix) and the rows of each sequence's own in pages (None: none)."""
-    B, Hq, Hkv, D, dt = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype]
-    rows = 0
+    B, Hq, Hkv, D, dt, dev = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype], _on(q)
+    rows, kp, vp = 0, None, None
     if K_pre is not None:
         rows = K_pre.shape[-2]
         shape = (Hkv, rows, D) if K_pre.dim() == 3 else (1, Hkv, rows, D)
-        _arg(K_pre, dt, shape, "K_pre")
-        _arg(V_pre, dt, shape, "V_pre")
+        kp = _arg(K_pre, dt, shape, "K_pre", dev)
+    if V_pre is not None:
+        vp = _arg(V_pre, dt, shape if kp else V_pre.shape, "V_pre", dev)
     if own is not None:
-        _check_pages(p, own)
-    _call("kvm_shared_attend", p, _arg(q, dt, (B, Hq, D), "q"), _ptr(K_pre), _ptr(V_pre), rows, _lengths(pre_len, Hkv, "pre_len"),
-          own, _arg(out, dt, (B, Hq, D), "out"), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
+        _check_pages(own, dev, B * Hkv, D, dt)
+    _call("kvm_shared_attend", p, _arg(q, dt, (B, Hq, D), "q", dev), kp, vp, rows, _lengths(pre_len, Hkv, "pre_len", dev), own,
+          _arg(out, dt, (B, Hq, D), "out", dev), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
 
 
 def kvm_cross_workspace_bytes(p: KvmParams, n_q: int, rows: int) -> int:
@@ -374,11 +388,12 @@ def kvm_cross_workspace_bytes(p: KvmParams, n_q: int, rows: int) -> int:
 def kvm_cross_attend(p: KvmParams, Q, K, V, length, O, lse, ws, O_in=None, lse_in=None, stats=None, stream=None) -> None:
     """Attention of Q [batch, n_q_heads, n_q, D] over K, V [batch, n_kv_heads, rows, D] (rows past `length` left out), joined with
     O_in, lse_in if given: O like Q, and the natural-log log-sum-exp [batch, n_q_heads, n_q]."""
-    B, Hq, Hkv, D, dt, n, rows = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype], Q.shape[2], K.shape[2]
-    _call("kvm_cross_attend", p, _arg(Q, dt, (B, Hq, n, D), "Q"), n, _arg(K, dt, (B, Hkv, rows, D), "K"),
-          _arg(V, dt, (B, Hkv, rows, D), "V"), rows, _lengths(length, B * Hkv, "length"), _arg(O_in, dt, (B, Hq, n, D), "O_in"),
-          _arg(lse_in, torch.float32, (B, Hq, n), "lse_in"), _arg(O, dt, (B, Hq, n, D), "O"),
-          _arg(lse, torch.float32, (B, Hq, n), "lse"), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
+    B, Hq, Hkv, D, dt, dev = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim, _TORCH_DTYPE[p.dtype], _on(Q)
+    n, rows = Q.shape[2], K.shape[2]
+    q_shape, k_shape, l_shape = (B, Hq, n, D), (B, Hkv, rows, D), (B, Hq, n)
+    _call("kvm_cross_attend", p, _arg(Q, dt, q_shape, "Q", dev), n, _arg(K, dt, k_shape, "K", dev), _arg(V, dt, k_shape, "V", dev), rows,
+          _lengths(length, B * Hkv, "length", dev), _arg(O_in, dt, q_shape, "O_in", dev), _arg(lse_in, torch.float32, l_shape, "lse_in", dev),
+          _arg(O, dt, q_shape, "O", dev), _arg(lse, torch.float32, l_shape, "lse", dev), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
 
 
 # ----------------------------------------------------------------------------- convenience

@@ -12,7 +12,9 @@
 //     of the product (16 keys at a time; the last ones' rows of V are zeroed in shared memory).
 // Bound by the exponentials and the softmax around them where there are many rows (see prefill_tc.cu for the clocks), by bandwidth where
 // a unit has one tile (64 KB of keys and values per step of about 2,800 clocks at an SM's share).
+#include <initializer_list>
 #include <mutex>
+#include <type_traits>
 
 #include "serve.cuh"
 #include "tc_common.cuh"
@@ -149,16 +151,10 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y)
-                 : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-
 template <int KCH>
 __global__ void __launch_bounds__(NTHREADS, 1)
 rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-               const __grid_constant__ CUtensorMap map_o, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ Args a) {
+               const __grid_constant__ Args a) {
     constexpr int D = KCH * KCHUNK;
     constexpr uint32_t TILE_BYTES = KCH * CHUNK_BYTES;
     extern __shared__ uint8_t smem_raw[];
@@ -181,6 +177,7 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (const CUtensorMap* map : {&map_q, &map_k, &map_v}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     grid_dependency_wait();
     Walk walk;
@@ -340,22 +337,24 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         uint32_t s_ph = 0, o_ph = 0;
         bool ok = true;
         Walk& mine = sh.walk[warp];
-        const Piece& p = sh.piece[warp];
         if (lane == 0) mine = walk;
+        // (lane 0 walks one piece ahead, so that what the lengths take to arrive is hidden)
+        bool ahead = lane == 0 && mine.next(sh.piece[warp]);
         for (;;) {
-            __syncwarp();                                    // (the last piece has been read)
-            bool more = false;
-            if (lane == 0) {
-                more = mine.next(sh.piece[warp]);
-                if (more && warp == 0 && p.k0 == 0) {        // (also where a wait gave up: whoever joins reads it)
-                    const unsigned long long s0 = mine.f - p.steps();
-                    const int item = p.u * mine.pairs + p.pair, last = (int)((s0 + p.nk - 1) / mine.q), count = last - (int)blockIdx.x + 1;
-                    a.st.pieces[item] = make_int4(count, count > 1 ? 2 * blockIdx.x + 1 : 2 * gridDim.x + item, 2 * blockIdx.x + 2, 0);
-                }
-            }
-            more = __any_sync(0xffffffffu, more);
+            const bool more = __any_sync(0xffffffffu, ahead);
             __syncwarp();
             if (!more) break;
+            const Piece p = sh.piece[warp];
+            const int pairs = mine.pairs, item = p.u * pairs + p.pair;
+            __syncwarp();
+            if (lane == 0) {
+                if (warp == 0 && p.k0 == 0) {                // (also where a wait gave up: whoever joins reads it)
+                    const unsigned long long s0 = mine.f - p.steps();
+                    const int last = (int)((s0 + p.nk - 1) / mine.q), count = last - (int)blockIdx.x + 1;
+                    a.st.pieces[item] = make_int4(count, count > 1 ? 2 * blockIdx.x + 1 : 2 * gridDim.x + item, 2 * blockIdx.x + 2, 0);
+                }
+                ahead = mine.next(sh.piece[warp]);
+            }
             const int tile = 2 * p.pair + g;
             if (tile >= a.tiles) continue;
             const int k0 = p.k0, k1 = p.k1, last_live = p.k1 == p.nk ? p.n - (p.nk - 1) * TILE : TILE;   // keys of the last step
@@ -378,8 +377,12 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 for (int c = 0; c < TILE; ++c) v[c] = __uint_as_float(vr[c]);
                 if (j == k1 - 1 && last_live < TILE) {       // keys that do not exist
 #pragma unroll
-                    for (int c = 0; c < TILE; ++c)
-                        if (c >= last_live) v[c] = -INFINITY;
+                    for (int q = 0; q < 4; ++q)
+                        if (last_live < q * 32 + 32) {
+#pragma unroll
+                            for (int c = q * 32; c < q * 32 + 32; ++c)
+                                if (c >= last_live) v[c] = -INFINITY;
+                        }
                 }
                 // p = 2^(x - m), summed in fp32, rounded to bf16 for the tensor core.  The first 32 keys are tried with the
                 // reference as it is, beside the search for the step's maximum: the warp's references move only when a row's
@@ -400,23 +403,26 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         pk[c >> 1] = __uint_as_float(r);
                     }
                 };
-                exponentials(0);
-                float mx4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                for (int c = 4; c + 7 < TILE; c += 8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) mx4[e] = fmax3(mx4[e], v[c + e], v[c + 4 + e]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], v[TILE - 4 + e]);
-                const float mx = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * a.scale2;
                 float alpha = 1.f;
-                if (__any_sync(0xffffffffu, mx > m + RESCALE_STEP)) {
+                bool again = false;
+#pragma unroll 1
+                for (;;) {                                   // (a loop, so that the instructions are there once)
+                    exponentials(0);
+                    if (again) break;
+                    float mx4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                    for (int c = 4; c + 7 < TILE; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mx4[e] = fmax3(mx4[e], v[c + e], v[c + 4 + e]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], v[TILE - 4 + e]);
+                    const float mx = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * a.scale2;
+                    if (!__any_sync(0xffffffffu, mx > m + RESCALE_STEP)) break;
                     if (mx > m) { alpha = ex2(m - mx); m = mx; }
                     sum[0] = sum[1] = 0ull;
                     rsum[0] = rsum[1] = rsum[2] = rsum[3] = 0.f;
-                    exponentials(0);
                     if (j > k0) {                            // (an S that is there says that the last P V is done)
-#pragma unroll
+#pragma unroll 1
                         for (int q = 0; q < D / 16; ++q) {
                             float o[16];
                             tmem_ld16(t_o + q * 16, o);
@@ -425,6 +431,7 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             tmem_st16(t_o + q * 16, o);
                         }
                     }
+                    again = true;
                 }
                 // (96 keys are handed over first: their products run while the last ones' P is made)
 #pragma unroll
@@ -443,11 +450,10 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 l = l * alpha + (s0 + s1);
                 lr = lr * alpha + ((rsum[0] + rsum[1]) + (rsum[2] + rsum[3]));
             }
-            // ---- the piece's end: 128 bytes of the warp's 32 rows at a time through shared memory
+            // ---- the piece's end
             ok = ok && mbar_wait(&sh.bar.o_full[g], o_ph, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             const bool direct = a.direct && p.whole();
-            const long long item = (long long)p.u * mine.pairs + p.pair;
             const long long slot = p.whole() ? 2ll * gridDim.x + item : Walk::slot(p);
             const long long srow = slot * a.st.rows + g * TILE + row;
             const int in = tile * TILE + row;                // (direct: row of the unit)
@@ -468,9 +474,39 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             o_ph ^= 1;
             tc_fence_after();
-            if (direct) {
-                const RowEnd end(m, l, lr, live ? a.out.lse_in : nullptr, orow);
+            // 128 bytes of the warp's 32 rows at a time through shared memory, 16 bytes per lane, so that four whole rows leave together.
+            // (In loops: unrolled, these instructions are fetched anew for every piece.)
+            const RowEnd end(m, l, lr, direct && live ? a.out.lse_in : nullptr, orow);
+            const int rows = min(32, direct ? a.m - tile * TILE - lq * 32 : a.gx * a.bx - lq * 32);      // (that exist; may be negative)
+            auto copy_out = [&](uint8_t* dst, auto pitch_of_rows) {          // the buffer's rows to dst, `pitch` apart
+                constexpr int pitch = decltype(pitch_of_rows)::value;
+                __syncwarp();
+                dst += (lane >> 3) * pitch + (lane & 7) * 16;
 #pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = i * 4 + (lane >> 3);
+                    const uint4 x = *reinterpret_cast<const uint4*>(buf + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+                    if (r < rows) *reinterpret_cast<uint4*>(dst + i * 4 * pitch) = x;
+                }
+                __syncwarp();
+            };
+            if (!direct) {
+                uint8_t* dst = (uint8_t*)a.st.o + (size_t)(srow - lane) * (D * 4);
+#pragma unroll 1
+                for (int q = 0; q < D / 32; ++q) {
+                    uint32_t o[32];
+                    tmem_ld32_issue(t_o + q * 32, o);
+                    tmem_ld_wait();
+                    tmem_ld_fence(o);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                    copy_out(dst + q * 128, std::integral_constant<int, D * 4>{});
+                }
+            } else {
+                uint8_t* dst = (uint8_t*)a.out.O + (size_t)(orow - lane) * (D * 2);
+                const uint64_t f2 = pack2(end.f, end.f);
+#pragma unroll 1
                 for (int kc = 0; kc < KCH; ++kc) {
                     uint32_t o[64];
                     tmem_ld32_issue(t_o + kc * 64, o);
@@ -478,44 +514,27 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     tmem_ld_wait();
                     tmem_ld_fence(o);
                     tmem_ld_fence(o + 32);
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        float y[8], x[8] = {};
-                        if (a.out.O_in && live)
+                        float y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2)
+                            unpack2(fmul2(pack2(__uint_as_float(o[c * 8 + e]), __uint_as_float(o[c * 8 + e + 1])), f2), y[e], y[e + 1]);
+                        if (end.f_in != 0.f) {               // (only where O_in is given)
+                            float x[8];
                             Vec<__nv_bfloat16>::unpack(__ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out.O_in + orow * D + kc * 64) + c), x);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = end_value(__uint_as_float(o[c * 8 + e]), end.f, x[e], end.f_in);
+                            for (int e = 0; e < 8; ++e) y[e] = fmaf(x[e], end.f_in, y[e]);
+                        }
                         *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = Vec<__nv_bfloat16>::pack(y);
                     }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0 && tile * TILE + lq * 32 < a.m) tma_store_3d(&map_o, buf, kc * KCHUNK, tile * TILE + lq * 32, p.u);
+                    copy_out(dst + kc * 128, std::integral_constant<int, D * 2>{});
                 }
-                tc_fence_before();                           // (the next piece's first P says that O has been read)
-                if (live) a.out.lse[orow] = end.lse;
-            } else {
-#pragma unroll
-                for (int q = 0; q < D / 32; ++q) {
-                    uint32_t o[32];
-                    tmem_ld32_issue(t_o + q * 32, o);
-                    tmem_ld_wait();
-                    tmem_ld_fence(o);
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0 && lq * 32 < a.gx * a.bx) tma_store_2d(&map_s, buf, q * 32, (int)(srow - lane));
-                }
-                tc_fence_before();
-                a.st.ml[srow] = make_float4(m, l, lr, 0.f);
             }
+            tc_fence_before();                               // (the next piece's first P says that O has been read)
+            if (!direct) a.st.ml[srow] = make_float4(m, l, lr, 0.f);
+            else if (live) a.out.lse[orow] = end.lse;
         }
-        if (lane == 0) bulk_wait();
     }
     __syncthreads();
     if (threadIdx.x == 0 && sh.abort_flag && a.stats) a.stats->status = KVM_E_DEVICE_TIMEOUT;
@@ -537,21 +556,8 @@ bool make_rows_map(CUtensorMap* map, const Queries& q, int units, int D, int gx,
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(q.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// The states' sums [rows, D] fp32, boxes of [32 rows, 32 channels].
-bool make_states_map(CUtensorMap* map, float* o, size_t rows, int D) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)D * 4};
-    cuuint32_t box[2] = {32, 32};
-    cuuint32_t estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, o, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int KCH>
-cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo,
-                     const CUtensorMap& ms, const Args& a, cudaStream_t st) {
+cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const Args& a, cudaStream_t st) {
     constexpr size_t smem = 1024 + (size_t)(2 + 2 * NST) * KCH * CHUNK_BYTES + NSOFT * 4096 + sizeof(Shared);
     static std::mutex mu;
     static bool ready[KVM_MAX_DEVICES] = {};
@@ -566,7 +572,7 @@ cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMa
             ready[dev] = true;
         }
     }
-    return launch_dependent(rows_tc_kernel<KCH>, dim3((unsigned)plan.grid), dim3(NTHREADS), smem, st, mq, mk, mv, mo, ms, a);
+    return launch_dependent(rows_tc_kernel<KCH>, dim3((unsigned)plan.grid), dim3(NTHREADS), smem, st, mq, mk, mv, a);
 }
 
 }  // namespace
@@ -589,16 +595,13 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
 
 cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                            kvm_stats* stats, cudaStream_t st) {
-    CUtensorMap mq, mk, mv, mo, ms;
-    if (!make_rows_map(&mq, q, units, s.D, plan.gx, plan.bx) || !make_map(&mk, k.K, units, k.rows, s.D) || !make_map(&mv, k.V, units, k.rows, s.D) ||
-        !make_states_map(&ms, states.o, (size_t)plan.slots * plan.slot_rows, s.D))
+    CUtensorMap mq, mk, mv;
+    if (!make_rows_map(&mq, q, units, s.D, plan.gx, plan.bx) || !make_map(&mk, k.K, units, k.rows, s.D) || !make_map(&mv, k.V, units, k.rows, s.D))
         return cudaErrorNotSupported;
-    mo = mq;                                    // (not used where nothing goes to the output)
-    if (plan.direct && !make_map(&mo, out.O, units, q.R, s.D, 32)) return cudaErrorNotSupported;
     Args a;
     a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.direct = plan.direct;
     a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats;
-    return s.D == 128 ? launch_t<2>(plan, mq, mk, mv, mo, ms, a, st) : launch_t<1>(plan, mq, mk, mv, mo, ms, a, st);
+    return s.D == 128 ? launch_t<2>(plan, mq, mk, mv, a, st) : launch_t<1>(plan, mq, mk, mv, a, st);
 }
 
 }  // namespace serve

@@ -272,6 +272,7 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     const Output o = {O, lse, O_in, lse_in};
     if (s.dtype == KVM_BF16) {
         if (launch_rows_tc(s, w.tc, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.tc.whole) return KVM_OK;
         return launch_join_items(s, s.U, m, w.states, len, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;

@@ -36,6 +36,7 @@ constexpr uint32_t CHUNK_BYTES = TILE * 128;            // [128 rows x 64 bf16]
 constexpr float RESCALE_STEP = 8.f;     // a row's reference moves when outgrown by this (log2 units): a weight is at most 2^8
 constexpr int P_FIRST = 96;             // keys of a step whose P is handed over first
 constexpr uint32_t S_COLS = TILE, O_COL0 = 2 * S_COLS;
+constexpr int NEAR = 64;
 constexpr float LOWEST = -1e30f;        // the reference before the first key (a row of -inf logits keeps it, and weighs nothing)
 
 struct __align__(8) Bars {
@@ -47,7 +48,7 @@ struct Args {
     Output out;
     States st;
     const int32_t* len;
-    int rows, units, tiles, direct;     // direct: an item in one piece goes to the output, else to slot 2 * gridDim.x + its number
+    int rows, units, tiles, whole, direct;      // direct: an item in one piece goes to the output, else to slot 2 * gridDim.x + its number
     int R, gx, bx, per_block;           // query rows of a block, a tile's box, tiles per block of more than 128 rows
     int m;                              // query rows of a unit
     float scale2;
@@ -62,18 +63,19 @@ struct Piece {
 };
 // A CTA's walk over its share of the steps.
 struct Walk {
-    const int32_t* len;
-    int rows, units, pairs;
-    int u, pair, n, nk;
+    const int32_t *len, *near;                  // near: the lengths of the first NEAR units of the share, in shared memory
+    int rows, units, pairs, u0;
+    int u, pair, n, nk, whole;                  // whole: items are not cut: a share is the items that begin in it
     unsigned long long q, f, f_end, start;      // steps per share; what is left of it; steps before the current item
     __device__ __forceinline__ int rows_of(int unit) const { return len ? max(0, min(__ldg(len + unit), rows)) : rows; }
+    __device__ __forceinline__ int next_rows(int unit) const { return unit - u0 < NEAR ? near[unit - u0] : rows_of(unit); }
     __device__ __forceinline__ static int tiles_of(int n) { return (n + TILE - 1) / TILE; }
     __device__ __forceinline__ bool next(Piece& p) {
         while (f < f_end) {
             if (f < start + nk) {
                 p.u = u; p.pair = pair; p.nk = nk; p.n = n;
                 p.k0 = (int)(f - start);
-                p.k1 = (int)(min(start + nk, f_end) - start);
+                p.k1 = whole ? nk : (int)(min(start + nk, f_end) - start);
                 f += p.k1 - p.k0;
                 return true;
             }
@@ -81,7 +83,7 @@ struct Walk {
             if (nk == 0 || ++pair == pairs) {
                 pair = 0;
                 if (++u >= units) return false;
-                n = rows_of(u);
+                n = next_rows(u);
                 nk = tiles_of(n);
             }
         }
@@ -96,7 +98,7 @@ struct alignas(16) Shared {
     uint32_t tmem_base;
     int abort_flag;
     unsigned long long wsum[NTHREADS / 32], start;
-    int unit;
+    int unit, near[NEAR];
     Walk walk[NSOFT];                   // of the softmax warps, whose registers hold the logits
     Piece piece[NSOFT];
 };
@@ -124,6 +126,8 @@ __device__ __forceinline__ bool take_share(Walk& w, Shared& sh) {
     w.q = (total + gridDim.x - 1) / gridDim.x;
     w.f = min(total, w.q * blockIdx.x);
     w.f_end = min(total, w.f + w.q);
+    w.u = w.u0 = w.n = w.nk = w.pair = 0;
+    w.start = 0;
     if (w.f == w.f_end) return false;
     if (before <= w.f && w.f < before + mine) {                    // true in exactly one thread
         unsigned long long st = before;
@@ -137,11 +141,15 @@ __device__ __forceinline__ bool take_share(Walk& w, Shared& sh) {
         sh.unit = id;
     }
     __syncthreads();
-    w.u = sh.unit;
-    w.n = w.rows_of(w.u);
+    w.u = w.u0 = sh.unit;
+    w.near = sh.near;
+    if (threadIdx.x < NEAR) sh.near[threadIdx.x] = w.rows_of(min(w.u + (int)threadIdx.x, w.units - 1));
+    __syncthreads();
+    w.n = sh.near[0];
     w.nk = Walk::tiles_of(w.n);
     w.pair = (int)((w.f - sh.start) / w.nk);
     w.start = sh.start + (unsigned long long)w.pair * w.nk;
+    if (w.whole && w.f > w.start) w.f = w.start + w.nk;            // the item that began before belongs to that share
     return true;
 }
 
@@ -151,10 +159,16 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
-template <int KCH>
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+template <int KCH, bool COMPACT>
 __global__ void __launch_bounds__(NTHREADS, 1)
 rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-               const __grid_constant__ Args a) {
+               const __grid_constant__ CUtensorMap map_o, const __grid_constant__ CUtensorMap map_s, const __grid_constant__ Args a) {
     constexpr int D = KCH * KCHUNK;
     constexpr uint32_t TILE_BYTES = KCH * CHUNK_BYTES;
     extern __shared__ uint8_t smem_raw[];
@@ -177,12 +191,12 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         }
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (const CUtensorMap* map : {&map_q, &map_k, &map_v}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        for (const CUtensorMap* map : {&map_q, &map_k, &map_v, &map_o, &map_s}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     grid_dependency_wait();
     Walk walk;
-    walk.len = a.len; walk.rows = a.rows; walk.units = a.units; walk.pairs = (a.tiles + 1) / 2;
-    if (!take_share(walk, sh)) return;
+    walk.len = a.len; walk.rows = a.rows; walk.units = a.units; walk.whole = a.whole; walk.pairs = (a.tiles + 1) / 2;
+    if (!take_share(walk, sh) && !(a.whole && a.direct && a.len)) return;
     if (a.gx * a.bx < TILE) {                              // rows of a Q tile that no copy fills: zeros
         for (int i = threadIdx.x; i < (int)(2 * TILE_BYTES / 16); i += NTHREADS) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0, 0, 0, 0);
         fence_proxy_async();
@@ -260,26 +274,22 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (last) umma_commit(&sh.bar.q_empty[g]);
             }
         };
-        // A piece's first logits of a tile come right after the tile's last P V of the piece before.
+        // A piece's first logits of a tile come right after the tile's last P V of the piece before (the walk starts with a piece of
+        // no steps).  The tiles take turns in a loop, so that the instructions are there once: they are fetched anew by every launch.
         Piece nx;
-        bool valid = walk.next(nx);
-        auto first_logits = [&](int g, int i, uint32_t x) {
-            if (2 * nx.pair + g >= a.tiles) return;
+        bool has_next = walk.next(nx);
+        p.u = p.pair = p.k0 = p.k1 = p.nk = p.n = 0;
+        auto next_piece_here = [&](int g, int i) {           // its first K and Q tiles are there; false: it has no such tile
+            if (2 * nx.pair + g >= a.tiles) return false;
             ok = ok && mbar_wait_warp(&sh.bar.k0_full, i & 1, abort_flag) && mbar_wait_warp(&sh.bar.q_full[g], (q_ph >> g) & 1, abort_flag);
-            if (!ok) return;
+            if (!ok) return false;
             q_ph ^= 1u << g;
             tc_fence_after();
-            logits(g, x, nx.steps() == 1);
+            return true;
         };
-        for (int i = 0; ok && valid; ++i) {
-            p = nx;
-            const int len = p.steps(), both = 2 * p.pair + 1 < a.tiles;
-            if (i == 0) {
-#pragma unroll
-                for (int g = 0; g < 2; ++g) first_logits(g, 0, 0u);
-                if (ok && elect_one()) umma_commit(&sh.bar.k0_done);
-            }
-            valid = walk.next(nx);
+        for (int i = 0;; ++i) {                              // (number of the piece after p)
+            const int len = p.steps(), both = len > 0 && 2 * p.pair + 1 < a.tiles;
+#pragma unroll 1
             for (int j = 0; ok && j < len; ++j) {
                 const uint32_t x = kv + (uint32_t)j, s = x % NST;
                 ok = mbar_wait_warp(&sh.bar.kv_full[s], (x / NST) & 1, abort_flag);
@@ -297,9 +307,9 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         __syncwarp();
                     }
                 }
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    if (!ok || (g && !both)) continue;
+#pragma unroll 1
+                for (int g = 0; g < 1 + both; ++g) {
+                    if (!ok) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {            // the first keys' products run while the last ones' P is made
                         ok = ok && mbar_wait_warp(&sh.bar.p_full[g][h], (p_ph >> g) & 1, abort_flag);
@@ -316,15 +326,39 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     }
                     if (!ok) break;
                     p_ph ^= 1u << g;
-                    if (j + 1 < len) logits(g, x + 1, j + 2 == len);
-                    else if (valid) first_logits(g, i + 1, kv + (uint32_t)len);
+                    const bool more = j + 1 < len;
+                    if (more || (has_next && next_piece_here(g, i))) logits(g, more ? x + 1 : kv + (uint32_t)len, more ? j + 2 == len : nx.steps() == 1);
                 }
                 if (ok && elect_one()) umma_commit(&sh.bar.kv_empty[s]);
             }
-            if (!both && ok && valid) first_logits(1, i + 1, kv + (uint32_t)len);
-            if (ok && valid && elect_one()) umma_commit(&sh.bar.k0_done);
+            if (!ok || !has_next) break;
+#pragma unroll 1
+            for (int g = len > 0 ? 1 + both : 0; g < 2; ++g)
+                if (next_piece_here(g, i)) logits(g, kv + (uint32_t)len, nx.steps() == 1);
+            if (!ok) break;
+            if (elect_one()) umma_commit(&sh.bar.k0_done);
             kv += (uint32_t)len;
+            p = nx;
+            has_next = walk.next(nx);
         }
+      } else if (warp == NSOFT + 3) {
+        // ============================== units without keys ==============================
+        // (where items are cut, the kernel that joins their pieces sees to these)
+        if (a.whole && a.direct && a.len)
+            for (int u = blockIdx.x; u < a.units; u += gridDim.x) {
+                if (walk.rows_of(u) > 0) continue;
+                for (int r = 0; r < a.m; ++r) {
+                    const long long at = (long long)u * a.m + r;
+                    const float z = a.out.lse_in ? a.out.lse_in[at] : -INFINITY;
+                    if (lane * 8 < D) {
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (z != -INFINITY) x = __ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out.O_in + at * D) + lane);
+                        reinterpret_cast<uint4*>((__nv_bfloat16*)a.out.O + at * D)[lane] = x;
+                    }
+                    __syncwarp();
+                    if (lane == 0) a.out.lse[at] = z;
+                }
+            }
       }
     } else {
         // ============================== softmax of tile g ==============================
@@ -350,7 +384,7 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (lane == 0) {
                 if (warp == 0 && p.k0 == 0) {                // (also where a wait gave up: whoever joins reads it)
                     const unsigned long long s0 = mine.f - p.steps();
-                    const int last = (int)((s0 + p.nk - 1) / mine.q), count = last - (int)blockIdx.x + 1;
+                    const int last = (int)((s0 + p.nk - 1) / mine.q), count = mine.whole ? 1 : last - (int)blockIdx.x + 1;
                     a.st.pieces[item] = make_int4(count, count > 1 ? 2 * blockIdx.x + 1 : 2 * gridDim.x + item, 2 * blockIdx.x + 2, 0);
                 }
                 ahead = mine.next(sh.piece[warp]);
@@ -366,36 +400,17 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (!ok) break;
                 s_ph ^= 1;
                 tc_fence_after();
-                uint32_t vr[TILE];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld32_issue(t_s + q * 32, vr + q * 32);
-                tmem_ld_wait();
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld_fence(vr + q * 32);
-                float v[TILE];
-#pragma unroll
-                for (int c = 0; c < TILE; ++c) v[c] = __uint_as_float(vr[c]);
-                if (j == k1 - 1 && last_live < TILE) {       // keys that do not exist
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (last_live < q * 32 + 32) {
-#pragma unroll
-                            for (int c = q * 32; c < q * 32 + 32; ++c)
-                                if (c >= last_live) v[c] = -INFINITY;
-                        }
-                }
-                // p = 2^(x - m), summed in fp32, rounded to bf16 for the tensor core.  The first 32 keys are tried with the
-                // reference as it is, beside the search for the step's maximum: the warp's references move only when a row's
-                // maximum has outgrown its own by RESCALE_STEP, seldom after the first step.
+                // p = 2^(x - m), summed in fp32, rounded to bf16 for the tensor core.
                 uint64_t sum[2] = {0ull, 0ull};
                 float rsum[4] = {0.f, 0.f, 0.f, 0.f};
                 float pk[16];                                // (two bf16 each)
-                auto exponentials = [&](int q) {
+                float alpha = 1.f;
+                auto exponentials = [&](const float* v) {    // of 32 keys
                     const uint64_t nm2 = pack2(-m, -m);
 #pragma unroll
                     for (int c = 0; c < 32; c += 2) {
                         float x0, x1;
-                        unpack2(ffma2(pack2(v[q * 32 + c], v[q * 32 + c + 1]), sc2, nm2), x0, x1);
+                        unpack2(ffma2(pack2(v[c], v[c + 1]), sc2, nm2), x0, x1);
                         const float e0 = ex2(x0), e1 = ex2(x1);
                         sum[(c >> 1) & 1] = fadd2(sum[(c >> 1) & 1], pack2(e0, e1));
                         const uint32_t r = Vec<__nv_bfloat16>::pack2(e0, e1);
@@ -403,46 +418,104 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         pk[c >> 1] = __uint_as_float(r);
                     }
                 };
-                float alpha = 1.f;
-                bool again = false;
-#pragma unroll 1
-                for (;;) {                                   // (a loop, so that the instructions are there once)
-                    exponentials(0);
-                    if (again) break;
-                    float mx4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-                    for (int c = 4; c + 7 < TILE; c += 8)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mx4[e] = fmax3(mx4[e], v[c + e], v[c + 4 + e]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], v[TILE - 4 + e]);
-                    const float mx = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * a.scale2;
-                    if (!__any_sync(0xffffffffu, mx > m + RESCALE_STEP)) break;
+                auto move_reference = [&](float mx) {        // of the rows that have outgrown theirs, and of all O
                     if (mx > m) { alpha = ex2(m - mx); m = mx; }
-                    sum[0] = sum[1] = 0ull;
-                    rsum[0] = rsum[1] = rsum[2] = rsum[3] = 0.f;
-                    if (j > k0) {                            // (an S that is there says that the last P V is done)
+                    if (j == k0) return;                     // (an S that is there says that the last P V is done)
 #pragma unroll 1
-                        for (int q = 0; q < D / 16; ++q) {
-                            float o[16];
-                            tmem_ld16(t_o + q * 16, o);
+                    for (int q = 0; q < D / 16; ++q) {
+                        float o[16];
+                        tmem_ld16(t_o + q * 16, o);
 #pragma unroll
-                            for (int c = 0; c < 16; ++c) o[c] *= alpha;
-                            tmem_st16(t_o + q * 16, o);
-                        }
+                        for (int c = 0; c < 16; ++c) o[c] *= alpha;
+                        tmem_st16(t_o + q * 16, o);
                     }
-                    again = true;
-                }
-                // (96 keys are handed over first: their products run while the last ones' P is made)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (q > 0) exponentials(q);
-                    tmem_st16(t_s + q * 16, pk);
-                    if (q == P_FIRST / 32 - 1 || q == 3) {
+                };
+                auto hand_over = [&](int q) {                // P of quarter q is in tensor memory
+                    if (q == P_FIRST / 32 - 1 || q == 3) {   // (96 keys first: their products run while the last ones' P is made)
                         tmem_st_wait();
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&sh.bar.p_full[g][q == 3]);
+                    }
+                };
+                const int live = j == k1 - 1 ? last_live : TILE;
+                if (COMPACT) {
+                    // Short shares: a quarter of the step at a time, read twice from tensor memory.  Three times less instructions to fetch
+                    // by a launch that executes them a few times only.
+                    auto load = [&](int q, float* v) {
+                        uint32_t r[32];
+                        tmem_ld32_issue(t_s + q * 32, r);
+                        tmem_ld_wait();
+                        tmem_ld_fence(r);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(r[c]);
+                        const int there = live - q * 32;     // keys that exist
+                        if (there < 32)
+#pragma unroll
+                            for (int c = 0; c < 32; ++c)
+                                if (c >= there) v[c] = -INFINITY;
+                    };
+                    float mx = -INFINITY, v[32];
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        load(q, v);
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2) mx = fmax3(mx, v[c], v[c + 1]);
+                    }
+                    mx *= a.scale2;
+                    if (__any_sync(0xffffffffu, mx > m + RESCALE_STEP)) move_reference(mx);
+#pragma unroll 1
+                    for (int q = 0; q < 4; ++q) {
+                        load(q, v);
+                        exponentials(v);
+                        tmem_st16(t_s + q * 16, pk);
+                        hand_over(q);
+                    }
+                } else {
+                    uint32_t vr[TILE];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_ld32_issue(t_s + q * 32, vr + q * 32);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_ld_fence(vr + q * 32);
+                    float v[TILE];
+#pragma unroll
+                    for (int c = 0; c < TILE; ++c) v[c] = __uint_as_float(vr[c]);
+                    if (live < TILE) {                       // keys that do not exist
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (live < q * 32 + 32) {
+#pragma unroll
+                                for (int c = q * 32; c < q * 32 + 32; ++c)
+                                    if (c >= live) v[c] = -INFINITY;
+                            }
+                    }
+                    // The first 32 keys are tried with the reference as it is, beside the search for the step's maximum: the warp's
+                    // references move only when a row's maximum has outgrown its own by RESCALE_STEP, seldom after the first step.
+                    bool again = false;
+#pragma unroll 1
+                    for (;;) {                               // (a loop, so that the instructions are there once)
+                        exponentials(v);
+                        if (again) break;
+                        float mx4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                        for (int c = 4; c + 7 < TILE; c += 8)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) mx4[e] = fmax3(mx4[e], v[c + e], v[c + 4 + e]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mx4[e] = fmaxf(mx4[e], v[TILE - 4 + e]);
+                        const float mx = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * a.scale2;
+                        if (!__any_sync(0xffffffffu, mx > m + RESCALE_STEP)) break;
+                        move_reference(mx);
+                        sum[0] = sum[1] = 0ull;
+                        rsum[0] = rsum[1] = rsum[2] = rsum[3] = 0.f;
+                        again = true;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (q > 0) exponentials(v + q * 32);
+                        tmem_st16(t_s + q * 16, pk);
+                        hand_over(q);
                     }
                 }
                 float s0, s1;
@@ -474,37 +547,27 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             o_ph ^= 1;
             tc_fence_after();
-            // 128 bytes of the warp's 32 rows at a time through shared memory, 16 bytes per lane, so that four whole rows leave together.
+            // 128 bytes of the warp's 32 rows at a time through shared memory to the copy engine, which takes them out beside the next
+            // piece (stored by the threads, 64 KB of two tiles hold the softmax up for 2,000 clocks more).
             // (In loops: unrolled, these instructions are fetched anew for every piece.)
             const RowEnd end(m, l, lr, direct && live ? a.out.lse_in : nullptr, orow);
-            const int rows = min(32, direct ? a.m - tile * TILE - lq * 32 : a.gx * a.bx - lq * 32);      // (that exist; may be negative)
-            auto copy_out = [&](uint8_t* dst, auto pitch_of_rows) {          // the buffer's rows to dst, `pitch` apart
-                constexpr int pitch = decltype(pitch_of_rows)::value;
-                __syncwarp();
-                dst += (lane >> 3) * pitch + (lane & 7) * 16;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = i * 4 + (lane >> 3);
-                    const uint4 x = *reinterpret_cast<const uint4*>(buf + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-                    if (r < rows) *reinterpret_cast<uint4*>(dst + i * 4 * pitch) = x;
-                }
-                __syncwarp();
-            };
             if (!direct) {
-                uint8_t* dst = (uint8_t*)a.st.o + (size_t)(srow - lane) * (D * 4);
 #pragma unroll 1
                 for (int q = 0; q < D / 32; ++q) {
                     uint32_t o[32];
                     tmem_ld32_issue(t_o + q * 32, o);
                     tmem_ld_wait();
                     tmem_ld_fence(o);
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
                         *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-                    copy_out(dst + q * 128, std::integral_constant<int, D * 4>{});
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0 && lq * 32 < a.gx * a.bx) tma_store_2d(&map_s, buf, q * 32, (int)(srow - lane));
                 }
             } else {
-                uint8_t* dst = (uint8_t*)a.out.O + (size_t)(orow - lane) * (D * 2);
                 const uint64_t f2 = pack2(end.f, end.f);
 #pragma unroll 1
                 for (int kc = 0; kc < KCH; ++kc) {
@@ -514,6 +577,8 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     tmem_ld_wait();
                     tmem_ld_fence(o);
                     tmem_ld_fence(o + 32);
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         float y[8];
@@ -528,13 +593,16 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         }
                         *reinterpret_cast<uint4*>(buf + lane * 128 + ((c ^ (lane & 7)) << 4)) = Vec<__nv_bfloat16>::pack(y);
                     }
-                    copy_out(dst + kc * 128, std::integral_constant<int, D * 2>{});
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0 && tile * TILE + lq * 32 < a.m) tma_store_3d(&map_o, buf, kc * KCHUNK, tile * TILE + lq * 32, p.u);
                 }
             }
             tc_fence_before();                               // (the next piece's first P says that O has been read)
             if (!direct) a.st.ml[srow] = make_float4(m, l, lr, 0.f);
             else if (live) a.out.lse[orow] = end.lse;
         }
+        if (lane == 0) bulk_wait();
     }
     __syncthreads();
     if (threadIdx.x == 0 && sh.abort_flag && a.stats) a.stats->status = KVM_E_DEVICE_TIMEOUT;
@@ -556,8 +624,21 @@ bool make_rows_map(CUtensorMap* map, const Queries& q, int units, int D, int gx,
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(q.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <int KCH>
-cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const Args& a, cudaStream_t st) {
+// The states' sums [rows, D] fp32, boxes of [32 rows, 32 channels].
+bool make_states_map(CUtensorMap* map, float* o, size_t rows, int D) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)D * 4};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, o, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int KCH, bool COMPACT>
+cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo,
+                     const CUtensorMap& ms, const Args& a, cudaStream_t st) {
     constexpr size_t smem = 1024 + (size_t)(2 + 2 * NST) * KCH * CHUNK_BYTES + NSOFT * 4096 + sizeof(Shared);
     static std::mutex mu;
     static bool ready[KVM_MAX_DEVICES] = {};
@@ -568,14 +649,17 @@ cudaError_t launch_t(const TcPlan& plan, const CUtensorMap& mq, const CUtensorMa
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev]) {
-            if ((e = cudaFuncSetAttribute(rows_tc_kernel<KCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+            if ((e = cudaFuncSetAttribute(rows_tc_kernel<KCH, COMPACT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
             ready[dev] = true;
         }
     }
-    return launch_dependent(rows_tc_kernel<KCH>, dim3((unsigned)plan.grid), dim3(NTHREADS), smem, st, mq, mk, mv, a);
+    return launch_dependent(rows_tc_kernel<KCH, COMPACT>, dim3((unsigned)plan.grid), dim3(NTHREADS), smem, st, mq, mk, mv, mo, ms, a);
 }
 
 }  // namespace
+
+// Steps of a CTA that cut items cost in all.  (128 heads x 1024 queries x 1075-1433 keys, 512 items of up to 12 steps: cut 126 us, whole 109.)
+constexpr int WHOLE = 12;
 
 // (Sizes only: the workspace is asked for without a device.  148 SMs, one CTA each.)
 TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
@@ -586,8 +670,12 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
     p.tiles = p.per_block ? N * p.per_block : (N + p.bx - 1) / p.bx;
     p.direct = direct;
     p.items = (p.tiles + 1) / 2;
-    const long long steps = (long long)units * p.items * ((rows + TILE - 1) / TILE);
+    const long long tiles = (rows + TILE - 1) / TILE, all = (long long)units * p.items, steps = all * tiles;
     p.grid = steps < 148 ? (int)steps : 148;
+    // Items stay whole where the fullest CTA then has at most WHOLE steps more than an equal share: what the states of cut items and their
+    // joining cost.
+    p.whole = (all + p.grid - 1) / p.grid * tiles * p.grid <= steps + WHOLE * p.grid;
+    p.compact = steps <= 24 * p.grid;
     p.slot_rows = p.tiles > 1 ? 2 * TILE : TILE;
     p.slots = 2ll * p.grid + (direct ? 0 : (long long)units * p.items);
     return p;
@@ -595,13 +683,17 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
 
 cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                            kvm_stats* stats, cudaStream_t st) {
-    CUtensorMap mq, mk, mv;
-    if (!make_rows_map(&mq, q, units, s.D, plan.gx, plan.bx) || !make_map(&mk, k.K, units, k.rows, s.D) || !make_map(&mv, k.V, units, k.rows, s.D))
+    CUtensorMap mq, mk, mv, mo, ms;
+    if (!make_rows_map(&mq, q, units, s.D, plan.gx, plan.bx) || !make_map(&mk, k.K, units, k.rows, s.D) || !make_map(&mv, k.V, units, k.rows, s.D) ||
+        !make_states_map(&ms, states.o, (size_t)plan.slots * plan.slot_rows, s.D))
         return cudaErrorNotSupported;
+    mo = mq;                                    // (not used where nothing goes to the output)
+    if (plan.direct && !make_map(&mo, out.O, units, q.R, s.D, 32)) return cudaErrorNotSupported;
     Args a;
-    a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.direct = plan.direct;
+    a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.whole = plan.whole; a.direct = plan.direct;
     a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats;
-    return s.D == 128 ? launch_t<2>(plan, mq, mk, mv, a, st) : launch_t<1>(plan, mq, mk, mv, a, st);
+    auto fn = s.D == 128 ? (plan.compact ? launch_t<2, true> : launch_t<2, false>) : (plan.compact ? launch_t<1, true> : launch_t<1, false>);
+    return fn(plan, mq, mk, mv, mo, ms, a, st);
 }
 
 }  // namespace serve

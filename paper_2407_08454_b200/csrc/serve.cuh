@@ -134,6 +134,7 @@ struct TcPlan {
     int gx, bx;                                 // rows of a query tile: bx blocks of gx rows
     int per_block, tiles, items;                // tiles of a block of more than 128 rows (else 0), tiles and items (pairs of tiles) of a unit
     int direct, grid, slot_rows;                // direct: an item in one piece goes to the output
+    int compact, whole;                         // few steps per CTA; items are not cut
     long long slots;
 };
 TcPlan tc_plan(int units, int R, int N, int rows, bool direct);

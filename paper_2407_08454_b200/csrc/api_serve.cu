@@ -41,6 +41,9 @@ int derive(const kvm_pages* c, bool sizes_only, Pages& o) {
     return KVM_OK;
 }
 
+// (Blocks of 16 rows are counted in 32 bits.)
+bool too_many(const Shape& s, const Pages& c) { return (long long)s.B * s.Hq * (c.room() / 16) >= (1ll << 31); }
+
 struct Carver {
     char* base;
     size_t off = 0;
@@ -80,10 +83,23 @@ States tc_states(const TcPlan& plan, int units, int D, int R, Carver& c) {
     return s;
 }
 
+// States of the parts of the paged kernel's items.
+States paged_states(const PagedPlan& plan, int D, Carver& c) {
+    States s = {};
+    s.rows = s.tile = plan.slot_rows;
+    s.items = plan.hg;
+    s.stride = 1;
+    s.o = (float*)c.take((size_t)plan.slots * plan.slot_rows * D * sizeof(float));
+    s.ml = (float4*)c.take((size_t)plan.slots * plan.slot_rows * sizeof(float4));
+    s.pieces = (int4*)c.take((size_t)plan.items * sizeof(int4));
+    return s;
+}
+
 // How a call of the decode attention is dealt, and what it needs of the workspace.
 struct SharedWork {
     bool pre, own;
     TcPlan pre_tc;
+    PagedPlan own_paged;
     SimtPlan pre_plan, own_plan;
     States pre_states, own_states;
     size_t bytes;
@@ -101,10 +117,8 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
         if (w.own || w.pre_plan.pieces > 1) w.pre_states = simt_states(w.pre_plan, s.Hkv, s.D, c);
     }
     if (w.own && s.dtype == KVM_BF16) {
-        w.own_plan.mt = s.G;
-        w.own_plan.items = 1;
-        w.own_plan.pieces = paged_pieces(s, own->room());
-        if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
+        w.own_paged = paged_plan(s, own->room(), w.pre);
+        w.own_states = paged_states(w.own_paged, s.D, c);
     } else if (w.own) {
         w.own_plan = simt_plan(s.U, s.G, own->room());
         if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
@@ -202,6 +216,7 @@ int kvm_shared_workspace_bytes(const kvm_params* p, int32_t pre_rows, const kvm_
     if (!bytes) return KVM_E_NULL;
     if (pre_rows < 0 || pre_rows > KVM_MAX_ROWS || (pre_rows == 0 && !own)) return KVM_E_SHAPE;
     if (own && (rc = derive(own, true, pg)) != KVM_OK) return rc;
+    if (own && too_many(s, pg)) return KVM_E_SHAPE;
     *bytes = plan_shared(s, pre_rows, own ? &pg : nullptr, nullptr).bytes;
     return KVM_OK;
 }
@@ -216,6 +231,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (!q || !out || !K_pre != !V_pre || (!K_pre && !own)) return KVM_E_NULL;
     if (K_pre ? (pre_rows < 1 || pre_rows > KVM_MAX_ROWS) : pre_rows != 0) return KVM_E_SHAPE;
     if (own && (rc = derive(own, false, pg)) != KVM_OK) return rc;
+    if (own && too_many(s, pg)) return KVM_E_SHAPE;
     if (misaligned(q) || misaligned(out) || (K_pre && (misaligned(K_pre) || misaligned(V_pre))) || (pre_len && misaligned(pre_len, 4)))
         return KVM_E_ALIGN;
     const SharedWork w = plan_shared(s, pre_rows, own ? &pg : nullptr, ws);
@@ -223,22 +239,21 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (misaligned(ws)) return KVM_E_ALIGN;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const Output o = {out, nullptr, nullptr, nullptr};
-    if (w.pre) {
-        const Queries qs = {q, s.G, s.Hq, s.G, s.B};
-        const Keys ks = {K_pre, V_pre, pre_len, pre_rows, nullptr, 0, 0, 0};
-        const cudaError_t e = s.dtype == KVM_BF16 ? launch_rows_tc(s, w.pre_tc, s.Hkv, qs, ks, w.pre_states, o, stats, st)
-                                                  : launch_rows_simt(s, w.pre_plan, s.Hkv, qs, ks, w.pre_states, o, stats, st);
-        if (e != cudaSuccess) return KVM_E_CUDA;
-    }
-    if (w.own) {
-        const Queries qs = {q, s.G, 0, s.G, 1};
-        const Keys ks = {pg.K, pg.V, pg.len, pg.room(), pg.table, pg.n_pages, pg.shift, pg.max_pages};
-        const cudaError_t e = s.dtype == KVM_BF16 ? launch_rows_paged(s, w.own_plan.pieces, q, ks, w.own_states, out, stats, st)
-                                                  : launch_rows_simt(s, w.own_plan, s.U, qs, ks, w.own_states, o, stats, st);
-        if (e != cudaSuccess) return KVM_E_CUDA;
+    const Queries pre_q = {q, s.G, s.Hq, s.G, s.B}, own_q = {q, s.G, 0, s.G, 1};
+    const Keys pre_k = {K_pre, V_pre, pre_len, pre_rows, nullptr, 0, 0, 0};
+    const Keys own_k = {pg.K, pg.V, pg.len, own ? pg.room() : 0, pg.table, pg.n_pages, pg.shift, pg.max_pages};
+    const int32_t* own_len = nullptr;               // (of items that a table tells of)
+    if (s.dtype == KVM_BF16) {
+        const Beside pre = {pre_len, w.pre ? s.Hkv : 0, pre_rows, w.pre_tc.items, 128}, mine = {pg.len, w.own ? s.U : 0, own_k.rows, w.own_paged.hg, 16};
+        if (w.pre && launch_rows_tc(s, w.pre_tc, s.Hkv, pre_q, pre_k, mine, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.own && launch_rows_paged(s, w.own_paged, q, own_k, pre, w.own_states, w.pre ? nullptr : out, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        own_len = pg.len;
+    } else {
+        if (w.pre && launch_rows_simt(s, w.pre_plan, s.Hkv, pre_q, pre_k, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.own && launch_rows_simt(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
     if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
-    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, nullptr, w.pre ? &w.pre_states : nullptr, pre_len, o, st) == cudaSuccess
+    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, own_len, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, o, st) == cudaSuccess
                ? KVM_OK
                : KVM_E_CUDA;
 }
@@ -271,13 +286,13 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     const Keys ks = {K, V, len, rows, nullptr, 0, 0, 0};
     const Output o = {O, lse, O_in, lse_in};
     if (s.dtype == KVM_BF16) {
-        if (launch_rows_tc(s, w.tc, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (launch_rows_tc(s, w.tc, s.U, qs, ks, Beside{}, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
         if (w.tc.whole) return KVM_OK;
         return launch_join_items(s, s.U, m, w.states, len, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
-    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
 }
 
 }  // extern "C"

@@ -91,12 +91,13 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
 // has no entry there).
 template <typename T, int D> __global__ void __launch_bounds__(JOIN_NT)
 join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
-            const Output out, long long rows, int m_rows, int Hkv, int G) {
+            int skip_whole, const Output out, long long rows, int m_rows, int Hkv, int G) {
     const long long w = (long long)blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
     grid_dependency_wait();
     if (w >= rows) return;
     const int u = (int)(w / m_rows), m = (int)(w % m_rows);
     Sum<D / 32> s;
+    bool done = false;                              // (by the kernel that had the item whole)
     auto add = [&](const States& st, const int32_t* len, int unit, int row_of_unit) {
         int item, row;
         st.find(row_of_unit, item, row);
@@ -105,12 +106,13 @@ join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, i
             add_pieces<D>(s, st, at * st.count, at * st.count + 1, st.count, row);
         } else if (!len || __ldg(len + unit) > 0) {
             const int4 pc = __ldcg(st.pieces + at);
-            add_pieces<D>(s, st, pc.y, pc.z, pc.x, row);
+            done = skip_whole && pc.x == 1;
+            if (!done) add_pieces<D>(s, st, pc.y, pc.z, pc.x, row);
         }
     };
     if (has_b) add(b, b_len, u % Hkv, u / Hkv * G + m);
     if (has_a) add(a, a_len, u, m);
-    store_row<T, D>(s, out, w);
+    if (!done) store_row<T, D>(s, out, w);
 }
 
 // Items of which most have gone to the output in one piece: a block per 32 rows of a tile, which looks at its item first.
@@ -137,13 +139,13 @@ join_items_kernel(const States a, const int32_t* __restrict__ len, const Output 
 }  // namespace
 
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
-                        const Output& out, cudaStream_t st) {
+                        int skip_whole, const Output& out, cudaStream_t st) {
     const long long rows = (long long)units * m, blocks = (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
     auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>)
                                   : (s.D == 128 ? join_kernel<float, 128> : join_kernel<float, 64>);
     return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, a_len, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
-                            b_len, out, rows, m, s.Hkv, s.G);
+                            b_len, skip_whole, out, rows, m, s.Hkv, s.G);
 }
 
 cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st) {

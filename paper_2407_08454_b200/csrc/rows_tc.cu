@@ -53,6 +53,7 @@ struct Args {
     int m;                              // query rows of a unit
     float scale2;
     kvm_stats* stats;
+    Beside own;                         // the kernel that runs beside this one
 };
 
 // A part of an item: key tiles [k0, k1) of `nk` for query tiles 2 * pair, 2 * pair + 1 of unit u.
@@ -97,14 +98,15 @@ struct alignas(16) Shared {
     Bars bar;
     uint32_t tmem_base;
     int abort_flag;
-    unsigned long long wsum[NTHREADS / 32], start;
+    long long wsum[NTHREADS / 32];
+    unsigned long long start;
     int unit, near[NEAR];
     Walk walk[NSOFT];                   // of the softmax warps, whose registers hold the logits
     Piece piece[NSOFT];
 };
 
 // This CTA's share, by a prefix sum over the units (all threads; false: nothing to do).
-__device__ __forceinline__ bool take_share(Walk& w, Shared& sh) {
+__device__ __forceinline__ bool take_share(Walk& w, const Beside& own, int D, Shared& sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int E = (w.units + NTHREADS - 1) / NTHREADS, i0 = min(w.units, (int)threadIdx.x * E), i1 = min(w.units, i0 + E);
     unsigned long long mine = 0;
@@ -115,16 +117,19 @@ __device__ __forceinline__ bool take_share(Walk& w, Shared& sh) {
         const unsigned long long t = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += t;
     }
-    if (lane == 31) sh.wsum[warp] = inc;
+    if (lane == 31) sh.wsum[warp] = (long long)inc;
     __syncthreads();
     unsigned long long total = 0, before = inc - mine;
 #pragma unroll
     for (int x = 0; x < NTHREADS / 32; ++x) {
-        if (x < warp) before += sh.wsum[x];
-        total += sh.wsum[x];
+        if (x < warp) before += (unsigned long long)sh.wsum[x];
+        total += (unsigned long long)sh.wsum[x];
     }
-    w.q = (total + gridDim.x - 1) / gridDim.x;
-    w.f = min(total, w.q * blockIdx.x);
+    // (beside another kernel the CTAs of the SMs that it gets have nothing to do)
+    unsigned ctas = gridDim.x;
+    if (own.units) ctas = min(ctas, (unsigned)prefix_sms((long long)total, block_sum<NTHREADS>(own.part(NTHREADS), sh.wsum), D));
+    w.q = (total + ctas - 1) / ctas;
+    w.f = blockIdx.x < ctas ? min(total, w.q * blockIdx.x) : total;
     w.f_end = min(total, w.f + w.q);
     w.u = w.u0 = w.n = w.nk = w.pair = 0;
     w.start = 0;
@@ -194,9 +199,10 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         for (const CUtensorMap* map : {&map_q, &map_k, &map_v, &map_o, &map_s}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     grid_dependency_wait();
+    grid_launch_dependents();                              // (the kernel beside this one begins, or the one that joins lies ready)
     Walk walk;
     walk.len = a.len; walk.rows = a.rows; walk.units = a.units; walk.whole = a.whole; walk.pairs = (a.tiles + 1) / 2;
-    if (!take_share(walk, sh) && !(a.whole && a.direct && a.len)) return;
+    if (!take_share(walk, a.own, D, sh) && !(a.whole && a.direct && a.len)) return;
     if (a.gx * a.bx < TILE) {                              // rows of a Q tile that no copy fills: zeros
         for (int i = threadIdx.x; i < (int)(2 * TILE_BYTES / 16); i += NTHREADS) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0, 0, 0, 0);
         fence_proxy_async();
@@ -671,7 +677,7 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
     p.direct = direct;
     p.items = (p.tiles + 1) / 2;
     const long long tiles = (rows + TILE - 1) / TILE, all = (long long)units * p.items, steps = all * tiles;
-    p.grid = steps < 148 ? (int)steps : 148;
+    p.grid = steps < SMS ? (int)steps : SMS;
     // Items stay whole where the fullest CTA then has at most WHOLE steps more than an equal share: what the states of cut items and their
     // joining cost.
     p.whole = (all + p.grid - 1) / p.grid * tiles * p.grid <= steps + WHOLE * p.grid;
@@ -681,8 +687,8 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
     return p;
 }
 
-cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
-                           kvm_stats* stats, cudaStream_t st) {
+cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const Beside& own, const States& states,
+                           const Output& out, kvm_stats* stats, cudaStream_t st) {
     CUtensorMap mq, mk, mv, mo, ms;
     if (!make_rows_map(&mq, q, units, s.D, plan.gx, plan.bx) || !make_map(&mk, k.K, units, k.rows, s.D) || !make_map(&mv, k.V, units, k.rows, s.D) ||
         !make_states_map(&ms, states.o, (size_t)plan.slots * plan.slot_rows, s.D))
@@ -691,7 +697,7 @@ cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const 
     if (plan.direct && !make_map(&mo, out.O, units, q.R, s.D, 32)) return cudaErrorNotSupported;
     Args a;
     a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.whole = plan.whole; a.direct = plan.direct;
-    a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats;
+    a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats; a.own = own;
     auto fn = s.D == 128 ? (plan.compact ? launch_t<2, true> : launch_t<2, false>) : (plan.compact ? launch_t<1, true> : launch_t<1, false>);
     return fn(plan, mq, mk, mv, mo, ms, a, st);
 }

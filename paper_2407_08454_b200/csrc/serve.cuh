@@ -116,6 +116,40 @@ __device__ __forceinline__ float end_value(float o, float f, float x, float f_in
     return f_in != 0.f ? fmaf(x, f_in, y) : y;
 }
 
+// A shared prefix's kernel and the one for the sequences' own rows run side by side, each on a part of the SMs: the first is busy
+// with products and exponentials while the second waits for memory.  Each finds out from the lengths how much there is for the other.
+constexpr int SMS = 148;
+struct Beside {
+    const int32_t* len;                         // nullable: all `rows`
+    int units, rows, per, tile;                 // the other kernel's units (0: it does not run), items of a unit, rows of a step
+    // What this thread of `threads` finds of the other's steps (to be summed over the block).
+    __device__ __forceinline__ long long part(int threads) const {
+        long long n = 0;
+        for (int i = threadIdx.x; i < units; i += threads) n += (long long)((len ? max(0, min(__ldg(len + i), rows)) : rows) + tile - 1) / tile * per;
+        return n;
+    }
+};
+// SMs for the prefix: both parts end at about the same time.  A step of the prefix (128 keys, up to 256 query rows) takes an SM 1.6 us,
+// 16 rows of K and V at the 80 GB/s that an SM gets through 0.05 us (D = 64) or 0.1 us; more than OWN_MOST SMs memory does not feed.
+constexpr int OWN_MOST = 80;
+__device__ __forceinline__ int prefix_sms(long long steps, long long blocks, int D) {
+    const float a = 1.6f * (float)steps, b = (D == 128 ? 0.1f : 0.05f) * (float)blocks;
+    if (blocks == 0) return SMS;
+    const int own = (int)(SMS * b / (a + b) + 0.5f);
+    return SMS - max(1, min(own, steps == 0 ? SMS - 1 : OWN_MOST));
+}
+template <int THREADS> __device__ __forceinline__ long long block_sum(long long v, long long* smem) {       // smem: a long long per warp
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) smem[threadIdx.x >> 5] = v;
+    __syncthreads();
+    long long t = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) t += smem[i];
+    return t;
+}
+
 cudaError_t launch_append(const Shape& s, const Pages& c, int32_t* len_out, int n_new, const int32_t* new_len, const int32_t* pos,
                           const uint64_t* turns, int neighbours, const void* q, const void* k, const void* v, const int64_t* strides,
                           void* q_out, kvm_stats* stats, cudaStream_t st);
@@ -138,18 +172,23 @@ struct TcPlan {
     long long slots;
 };
 TcPlan tc_plan(int units, int R, int N, int rows, bool direct);
-cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
-                           kvm_stats* stats, cudaStream_t st);
+cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const Queries& q, const Keys& k, const Beside& own, const States& states,
+                           const Output& out, kvm_stats* stats, cudaStream_t st);
 
 // Decode attention over a paged cache (bf16), one query per sequence: rows_paged.cu.
-int paged_pieces(const Shape& s, int rows);
-cudaError_t launch_rows_paged(const Shape& s, int pieces, const void* q, const Keys& k, const States& states, void* out, kvm_stats* stats,
-                              cudaStream_t st);
+struct PagedPlan {
+    int hg, items, grid, slot_rows;             // groups of up to 8 heads per unit; items = units x groups
+    long long slots;
+};
+PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix);
+cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Beside& pre, const States& states, void* out,
+                              kvm_stats* stats, cudaStream_t st);
 
 // Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
 // unit = h and row = b * G + g, of `b` (a shared prefix).
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
-                        const Output& out, cudaStream_t st);
+                        int skip_whole, const Output& out, cudaStream_t st);
+// skip_whole: rows of items in one piece are in the output already.
 // The same for the tensor-core kernel's items [units][items] of m rows a unit, of which those in one piece are in the output already.
 cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st);
 

@@ -316,7 +316,7 @@ int kvm_attend(const kvm_params* p, const void* q, const void* K, const void* V,
  *   K, V   device [n_pages, page_rows, D] in p->dtype, 16-byte aligned
  *   table  device [U, max_pages] i32: the pages of each unit in order; entries past its rows are not read
  *   len    device [U] i32: rows that each unit holds
- *   page_rows  a power of two from 16 to 4096
+ *   page_rows  a power of two from 16 to 4096; n_pages * page_rows < 2^31, max_pages * page_rows <= KVM_MAX_ROWS
  * A row whose page number lies outside [0, n_pages) does not exist: it is neither written nor attended to, and
  * kvm_stats.status says KVM_E_PAGE.  Lengths below 0 count as 0, above max_pages * page_rows as that.  A page that two units
  * share is read by both; appending to it is the caller's mistake (the rows written last stay).

@@ -29,6 +29,7 @@ int derive(const kvm_params* p, Shape& s) {
 int derive(const kvm_pages* c, bool sizes_only, Pages& o) {
     if (c->page_rows < 16 || c->page_rows > 4096 || (c->page_rows & (c->page_rows - 1))) return KVM_E_SHAPE;
     if (c->n_pages < 1 || c->max_pages < 1 || (long long)c->max_pages * c->page_rows > KVM_MAX_ROWS) return KVM_E_SHAPE;
+    if ((long long)c->n_pages * c->page_rows >= (1ll << 31)) return KVM_E_SHAPE;
     if (c->reserved != 0) return KVM_E_PARAM;
     if (!sizes_only) {
         if (!c->K || !c->V || !c->table || !c->len) return KVM_E_NULL;

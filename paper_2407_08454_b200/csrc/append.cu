@@ -37,10 +37,11 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
     constexpr int N = Vec<T>::N, LPT = D / (2 * N), TPB = APPEND_NT / LPT;      // lanes per token, tokens per block
     const int lane = threadIdx.x % LPT;
     const long long tokens = (long long)a.B * a.T, x = (long long)blockIdx.x * TPB + threadIdx.x / LPT;
-    if (x >= tokens) return;
+    if (x >= tokens) return;                    // (leaving early counts as letting the next kernel lie ready)
     const int b = (int)(x / a.T), t = (int)(x % a.T);
     const int o0 = NEIGHBOURS ? lane * 2 * N : lane * N, o1 = NEIGHBOURS ? o0 + N : o0 + D / 2;
     grid_dependency_wait();
+    grid_launch_dependents();
 
     float cs[N], sn[N];
     if (a.turns) {

@@ -9,41 +9,85 @@ namespace {
 
 constexpr int JOIN_NT = 128;
 
+// A row's pieces in one set of states: `count` of them, in slots first, second, second + stride, ...
+struct Pieces {
+    int count, first, second, stride;
+    const float* o;                             // the row's sums in slot 0, and how far slots lie apart (rows)
+    const float4* ml;
+    int pitch;
+    __device__ __forceinline__ long long at(int i) const { return (long long)(i == 0 ? first : second + (i - 1) * stride) * pitch; }
+};
+template <int D> __device__ __forceinline__ Pieces pieces_of(const States& st, const int32_t* len, int unit, int m) {
+    int item, row;
+    st.find(m, item, row);
+    const int at = unit * st.items + item;
+    Pieces p;
+    p.stride = st.stride;
+    p.pitch = st.rows;
+    p.o = st.o + (size_t)row * D;
+    p.ml = st.ml + row;
+    if (st.count > 0) {
+        p.count = st.count;
+        p.first = at * st.count;
+        p.second = p.first + 1;
+    } else {                                    // (both reads leave together; a unit without keys has no entry in the table)
+        const int n = len ? __ldg(len + unit) : 1;
+        const int4 pc = __ldcg(st.pieces + at);
+        p.count = n > 0 ? pc.x : 0;
+        p.first = pc.y;
+        p.second = pc.z;
+    }
+    return p;
+}
+
 template <int E> struct Sum {                   // E channels of a row
-    float m = -INFINITY, l = 0.f, lr = 0.f, o[E] = {};
+    float m, l, lr, o[E];
 };
 
-template <int D, int BATCH>
-__device__ __forceinline__ void add_batches(Sum<D / 32>& s, const States& st, long long first, long long second, int count, int row) {
-    constexpr int E = D / 32;
-    const int lane = threadIdx.x & 31;
+// One loop over the pieces of both sets, BATCH at a time so that their loads leave together.  (Short code: a launch of a few warps spends
+// most of its time on fetching instructions.  With a copy of the loop for each set, and one for few and one for many pieces, 12.5 us for
+// 32 rows of 12 pieces.)
+template <int D> __device__ __forceinline__ Sum<D / 32> sum_pieces(const Pieces& a, const Pieces& b) {
+    constexpr int BATCH = 8, E = D / 32;
+    const int lane = threadIdx.x & 31, count = a.count + b.count;
+    Sum<E> s;
+    s.m = -INFINITY;
+    s.l = s.lr = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s.o[e] = 0.f;
+#pragma unroll 1
     for (int i0 = 0; i0 < count; i0 += BATCH) {
         float4 z[BATCH];
         float x[BATCH][E], mn = s.m;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const bool in = i0 + i < count;
-            const long long slot = i0 + i == 0 ? first : second + (long long)(i0 + i - 1) * st.stride;
-            const long long r = (in ? slot : first) * st.rows + row;
-            z[i] = __ldcg(st.ml + r);
-            if (E == 4) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(st.o + r * D) + lane);
-                x[i][0] = v.x; x[i][1] = v.y; x[i][E - 2] = v.z; x[i][E - 1] = v.w;
-            } else {
-                const float2 v = __ldcg(reinterpret_cast<const float2*>(st.o + r * D) + lane);
-                x[i][0] = v.x; x[i][1] = v.y;
-            }
-            if (!in) z[i].x = -INFINITY;
-            mn = fmaxf(mn, z[i].x);
-        }
-        const float a = rescale2(s.m, mn);
-        s.l *= a; s.lr *= a;
+            const int k = i0 + i;
+            const bool in_a = k < a.count;
+            const long long r = in_a ? a.at(k) : b.at(k - a.count);
+            z[i] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) s.o[e] *= a;
+            for (int e = 0; e < E; ++e) x[i][e] = 0.f;
+            if (k < count) {
+                z[i] = __ldcg((in_a ? a.ml : b.ml) + r);
+                const float* o = (in_a ? a.o : b.o) + r * D;
+                if (E == 4) {
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(o) + lane);
+                    x[i][0] = v.x; x[i][1] = v.y; x[i][E - 2] = v.z; x[i][E - 1] = v.w;
+                } else {
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(o) + lane);
+                    x[i][0] = v.x; x[i][1] = v.y;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) mn = fmaxf(mn, z[i].x);
+        const float f = rescale2(s.m, mn);
+        s.l *= f; s.lr *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s.o[e] *= f;
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            if (i0 + i >= count) break;
-            // (an empty state weighs nothing; a state that gave up is NaN whatever its reference says)
+            // (an empty state weighs nothing, whatever it holds; one that gave up is NaN whatever its reference says)
             const float w = z[i].y == 0.f ? 0.f : rescale2(z[i].x, mn);
             s.l = fmaf(z[i].y, w, s.l);
             s.lr = fmaf(z[i].z, w, s.lr);
@@ -53,14 +97,7 @@ __device__ __forceinline__ void add_batches(Sum<D / 32>& s, const States& st, lo
         }
         s.m = mn;
     }
-}
-
-// (Two pieces are what most cut items of a large problem have, and the loads of absent ones would not be free; a decode batch
-// over one prefix has about twenty.)
-template <int D>
-__device__ __forceinline__ void add_pieces(Sum<D / 32>& s, const States& st, long long first, long long second, int count, int row) {
-    if (count <= 2) add_batches<D, 2>(s, st, first, second, count, row);
-    else add_batches<D, 8>(s, st, first, second, count, row);
+    return s;
 }
 
 // The row's sums to the output (row w).
@@ -87,52 +124,40 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
     if (out.lse && lane == 0) out.lse[w] = end.lse;
 }
 
-// Row m of output unit u from one or two sets of states.  len: of the units whose pieces a table tells of (a unit without keys
-// has no entry there).
+// Row m of output unit u from one or two sets of states.  len: of the units whose pieces a table tells of.
 template <typename T, int D> __global__ void __launch_bounds__(JOIN_NT)
 join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
-            int skip_whole, const Output out, long long rows, int m_rows, int Hkv, int G) {
-    const long long w = (long long)blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
+            int skip_whole, const Output out, int rows, int m_rows, int Hkv, int G) {
+    const int w = blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
     grid_dependency_wait();
+    grid_launch_dependents();
     if (w >= rows) return;
-    const int u = (int)(w / m_rows), m = (int)(w % m_rows);
-    Sum<D / 32> s;
-    bool done = false;                              // (by the kernel that had the item whole)
-    auto add = [&](const States& st, const int32_t* len, int unit, int row_of_unit) {
-        int item, row;
-        st.find(row_of_unit, item, row);
-        const long long at = (long long)unit * st.items + item;
-        if (st.count > 0) {
-            add_pieces<D>(s, st, at * st.count, at * st.count + 1, st.count, row);
-        } else if (!len || __ldg(len + unit) > 0) {
-            const int4 pc = __ldcg(st.pieces + at);
-            done = skip_whole && pc.x == 1;
-            if (!done) add_pieces<D>(s, st, pc.y, pc.z, pc.x, row);
-        }
-    };
-    if (has_b) add(b, b_len, u % Hkv, u / Hkv * G + m);
-    if (has_a) add(a, a_len, u, m);
-    if (!done) store_row<T, D>(s, out, w);
+    const int u = w / m_rows, m = w - u * m_rows;
+    Pieces pa = {}, pb = {};
+    if (has_a) pa = pieces_of<D>(a, a_len, u, m);
+    if (has_b) pb = pieces_of<D>(b, b_len, u % Hkv, u / Hkv * G + m);
+    if (skip_whole && pa.count == 1) return;                       // (by the kernel that had the item whole)
+    store_row<T, D>(sum_pieces<D>(pa, pb), out, w);
 }
 
-// Items of which most have gone to the output in one piece: a block per 32 rows of a tile, which looks at its item first.
-// (A warp per row of the output took 44 us for 131,072 rows of which three in ten had pieces; a block per 32 rows XX.)
+// Items of which most have gone to the output in one piece: a block per ITEM_ROWS rows of a tile, which looks at its item first.
+// (A warp per row of the output took 44 us for 131,072 rows of which three in ten had pieces.)
 template <typename T, int D, int ITEM_ROWS> __global__ void __launch_bounds__(JOIN_NT)
 join_items_kernel(const States a, const int32_t* __restrict__ len, const Output out, int m_rows) {
     const int per = a.rows / ITEM_ROWS, part = blockIdx.x % per, at = blockIdx.x / per, u = at / a.items;
     const int m0 = (at % a.items) * a.rows + part * ITEM_ROWS;     // (tiles of an item follow one another in the unit)
     grid_dependency_wait();
+    grid_launch_dependents();
     if (m0 >= m_rows) return;
-    int4 pc = make_int4(0, 0, 0, 0);
-    if (!len || __ldg(len + u) > 0) {
-        pc = __ldcg(a.pieces + at);
-        if (pc.x == 1) return;
-    }
+    const int n = len ? __ldg(len + u) : 1;
+    const int4 pc = __ldcg(a.pieces + at);
+    if (n > 0 && pc.x == 1) return;
+    Pieces p = {n > 0 ? pc.x : 0, pc.y, pc.z, a.stride, a.o, a.ml, a.rows}, none = {};
 #pragma unroll 1
     for (int r = threadIdx.x >> 5; r < ITEM_ROWS && m0 + r < m_rows; r += JOIN_NT / 32) {
-        Sum<D / 32> s;
-        add_pieces<D>(s, a, pc.y, pc.z, pc.x, part * ITEM_ROWS + r);
-        store_row<T, D>(s, out, (long long)u * m_rows + m0 + r);
+        p.o = a.o + (size_t)(part * ITEM_ROWS + r) * D;
+        p.ml = a.ml + part * ITEM_ROWS + r;
+        store_row<T, D>(sum_pieces<D>(p, none), out, (long long)u * m_rows + m0 + r);
     }
 }
 
@@ -141,11 +166,11 @@ join_items_kernel(const States a, const int32_t* __restrict__ len, const Output 
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
                         int skip_whole, const Output& out, cudaStream_t st) {
     const long long rows = (long long)units * m, blocks = (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    if (rows > 0x7fffffffll) return cudaErrorInvalidValue;
     auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>)
                                   : (s.D == 128 ? join_kernel<float, 128> : join_kernel<float, 64>);
     return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, a_len, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
-                            b_len, skip_whole, out, rows, m, s.Hkv, s.G);
+                            b_len, skip_whole, out, (int)rows, m, s.Hkv, s.G);
 }
 
 cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st) {

@@ -1,24 +1,30 @@
 // Decode attention over the rows of a paged cache (bf16): one query per sequence, the G query heads of a KV head together.
 //   S = K q^T  (16 rows x 8 heads per chain of products),  O^T += V^T P  (16 channels x 8 heads), on warp-level matrix products:
-// the work is a stream of K and V past a handful of queries, bound by bandwidth, and these need neither shared memory nor a barrier
-// between the two products.  Rows come from memory straight into the operands' registers, 16 bytes per load:
-//   - the contraction over channels may run in any order, so the 8 channels that a lane's load brings are the ones that it holds of
-//     two products' operands (four lanes read 64 bytes of a row, the q operand is dealt alike);
-//   - V^T wants pairs of rows for one channel: a lane loads 8 channels of rows 2t, 2t + 1, 2t + 8, 2t + 9 and interleaves them, and the
-//     product of number j takes channel j of every lane's 8 as its 16 channels.
+// the work is a stream of K and V past a handful of queries, bound by bandwidth, and these need neither tensor memory nor a barrier
+// between the two products.
 // Work is dealt to warps: the list of all units' blocks of 16 rows, in equal shares, so that neither lengths that differ nor units that are
-// short leave any idle (a block of four warps per unit and piece of it took 26 us for 512 units of 292 rows, 76 MB).  Twelve warps to
-// an SM, 8 KB in flight for each: the next block's keys are asked for when the keys have been used, and so the values, across the
-// ends of units.  16 rows never cross a page (pages are powers of two from 16); page numbers are read a block ahead of the rows.
+// short leave any idle (a block of four warps per unit and piece of it took 26 us for 512 units of 292 rows, 76 MB; this XX).
+// A warp copies its own blocks into a ring of its own (TMA, 128-byte swizzle, so that ldmatrix meets no bank conflict), STAGES ahead
+// across the ends of units, and waits for nobody else: 192 KB are in flight per SM.  (Straight from memory into the operands'
+// registers, 8 KB in flight for each of twelve warps: as fast on all SMs, but half the rate per SM, which counts beside a prefix.)
+// 16 rows never cross a page (pages are powers of two from 16); page numbers are read a block ahead of the copies.
 // A unit's part of a share leaves its state, which another kernel joins (a unit that is whole may go to the output).
 // Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones.
+#include <mutex>
+
 #include "serve.cuh"
+#include "tc_common.cuh"
 
 namespace kvm {
 namespace serve {
 namespace {
 
-constexpr int WARPS = 4, NT = WARPS * 32, HEADS = 8, PER_SM = 3;
+using namespace tc;
+
+constexpr int WARPS = 4, NT = WARPS * 32, HEADS = 8, PER_SM = 2;
+constexpr int STAGE_ROWS = 16;
+template <int D> constexpr int stages() { return D == 128 ? 3 : 6; }      // 24 KB per warp
+constexpr int RING_BYTES = 3 * 8192;
 constexpr int MIN_BLOCKS = 2;               // fewest blocks of a warp's share (bounds the number of parts)
 constexpr int KEPT = 1024;                  // items whose lengths are kept in shared memory
 constexpr float LOWEST = -1e30f, RESCALE_STEP = 8.f;
@@ -43,12 +49,18 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y) : "memory");
+}
 
 // Where a warp stands in the list of blocks.
 struct Cursor {
@@ -56,13 +68,25 @@ struct Cursor {
     int left;                               // blocks of the share from this one on; 0: past the end
 };
 
-template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel(const Args a) {
-    constexpr int KC = D / 32;                      // 16-byte loads per key row and lane
-    constexpr int VC = D / 64;                      // ... per value row
+template <int D> __global__ void __launch_bounds__(NT, PER_SM)
+rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ Args a) {
+    constexpr int STAGES = stages<D>(), KCH = D / 64;              // 64-channel (128-byte) column chunks
+    constexpr uint32_t CHUNK = STAGE_ROWS * 128, TENSOR = KCH * CHUNK, STAGE = 2 * TENSOR;       // bytes of a chunk, of K or V, of a stage
     constexpr int MT = D / 16;                      // products of 16 channels
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full[WARPS][STAGES];
+    __shared__ volatile int s_bad;
     __shared__ long long sm_all[WARPS];
     __shared__ int sm_sum[WARPS], sm_start, sm_item, sm_rows[KEPT];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    if (threadIdx.x == 0) {
+        for (int w = 0; w < WARPS; ++w)
+            for (int i = 0; i < STAGES; ++i) mbar_init(&full[w][i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        s_bad = 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
     if (!a.pre.units) grid_dependency_wait();       // (beside a prefix: when that kernel lets this one begin, what comes before it is done)
     grid_launch_dependents();                       // (who joins is there when this kernel ends, and waits for that)
 
@@ -138,40 +162,37 @@ template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel
         auto page_of = [&](const Cursor& c) {
             return c.left > 0 ? __ldg(a.k.table + (size_t)(c.item / a.HG) * a.k.max_pages + (c.b >> bshift)) : -1;
         };
-        uint4 qf[KC], kf[2][KC], vf[4][VC];
+        const uint32_t ring = ((smem_u32(smem_raw) + 1023u) & ~1023u) + warp * RING_BYTES;
+        uint32_t qf[D / 16][2];                     // q^T as the second operand: channels 2 tig.. (+ 8) of head gid
         auto load_q = [&](const Cursor& c) {
             const int u = c.item / a.HG, h = (c.item - u * a.HG) * HEADS + gid;
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q + ((size_t)u * a.G + h) * D) + tig;
 #pragma unroll
-            for (int i = 0; i < KC; ++i)
-                qf[i] = h < a.G ? ldg16(a.q + ((size_t)u * a.G + h) * D + i * 32 + tig * 8) : make_uint4(0, 0, 0, 0);
+            for (int ks = 0; ks < D / 16; ++ks) {
+                qf[ks][0] = h < a.G ? __ldg(p + ks * 8) : 0u;
+                qf[ks][1] = h < a.G ? __ldg(p + ks * 8 + 4) : 0u;
+            }
         };
-        // (a page that does not exist is not touched: what the registers hold is masked)
-        auto load_k = [&](const Cursor& c, int page) {
-            if (c.left <= 0 || (unsigned)page >= (unsigned)a.k.n_pages) return;
-            const __nv_bfloat16* p = (const __nv_bfloat16*)a.k.K + ((((size_t)page << a.k.shift) + ((c.b & bmask) << 4) + gid) * D + tig * 8);
+        // (a page that does not exist is not touched: the stage is full at once, and what it holds is masked)
+        auto issue = [&](const Cursor& c, int page, int s) {
+            if (c.left <= 0 || lane != 0) return;
+            uint64_t* bar = &full[warp][s];
+#ifdef KVM_TEST_DROP_ATTEND_STAGE
+            if (blockIdx.x == KVM_TEST_DROP_CTA && warp == 0 && c.left == w1 - w0 - (KVM_TEST_DROP_ATTEND_STAGE)) return;   // test build only: this block never arrives
+#endif
+            if ((unsigned)page >= (unsigned)a.k.n_pages) {
+                mbar_arrive(bar);
+                return;
+            }
+            mbar_expect_tx(bar, STAGE);
+            const int row = (page << a.k.shift) + ((c.b & bmask) << 4);
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int i = 0; i < KC; ++i) kf[r][i] = ldg16(p + r * 8 * D + i * 32);
+            for (int i = 0; i < KCH; ++i) {
+                tma_load_2d(ring + s * STAGE + i * CHUNK, &map_k, bar, i * 64, row);
+                tma_load_2d(ring + s * STAGE + TENSOR + i * CHUNK, &map_v, bar, i * 64, row);
+            }
         };
-        auto load_v = [&](const Cursor& c, int page) {
-            if (c.left <= 0 || (unsigned)page >= (unsigned)a.k.n_pages) return;
-            const __nv_bfloat16* p = (const __nv_bfloat16*)a.k.V + ((((size_t)page << a.k.shift) + ((c.b & bmask) << 4) + 2 * tig) * D + gid * 8);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < VC; ++i) vf[r][i] = ldg16(p + ((r & 1) + (r >> 1) * 8) * D + i * 64);
-        };
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int i = 0; i < KC; ++i) kf[r][i] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < VC; ++i) vf[r][i] = make_uint4(0, 0, 0, 0);
-
-        float o[MT][4];                             // channels of the lane's rows of product j, heads 2 tig, 2 tig + 1
+        float o[MT][4];                             // channels of product j: 16 j + gid (+ 8), heads 2 tig, 2 tig + 1
         float m[2], l[2];
         auto reset = [&]() {
 #pragma unroll
@@ -182,24 +203,39 @@ template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel
             l[0] = l[1] = 0.f;
         };
         reset();
-        int page = page_of(cur), b_first = cur.b;   // b_first: the part's first block
-        Cursor nxt = advance(cur);
-        int page_next = page_of(nxt);
-        load_k(cur, page);
-        load_v(cur, page);
+        const int krow = lane & 15, kpc = lane >> 4, vrow = (lane & 7) + ((lane >> 4) << 3), vpc = (lane >> 3) & 1;
+        int b_first = cur.b;                        // the part's first block
+        Cursor ld = cur;                            // the next block to copy
+        int page = page_of(ld);
+        uint32_t there_bits = 0, phase = 0;         // of the stages: whether the page exists, the barrier's parity
+        auto copy_next = [&](int s) {
+            issue(ld, page, s);
+            there_bits = (there_bits & ~(1u << s)) | ((unsigned)page < (unsigned)a.k.n_pages ? 1u << s : 0u);
+            ld = advance(ld);
+            page = page_of(ld);
+        };
+#pragma unroll 1
+        for (int s = 0; s < STAGES; ++s) copy_next(s);
         load_q(cur);
+        int s = 0;
+        bool ok = true;
         while (cur.left > 0) {
-            const bool there = (unsigned)page < (unsigned)a.k.n_pages;
+            const bool there = there_bits >> s & 1;
             const int live = there ? cur.n - cur.b * 16 : 0;       // rows that exist
             if (!there && a.stats) a.stats->status = KVM_E_PAGE;
+            const Cursor nxt = advance(cur);
             const bool last = nxt.left <= 0 || nxt.item != cur.item;
+            // (the warp's own copies always complete; a wait that ran out all the same makes the part NaN)
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(&full[warp][s], phase >> s & 1, &s_bad));
+            phase ^= 1u << s;
+            const uint32_t kb = ring + s * STAGE, vb = kb + TENSOR;
             float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < KC; ++i) {
-                mma16816(c0, kf[0][i].x, kf[1][i].x, kf[0][i].y, kf[1][i].y, qf[i].x, qf[i].y);
-                mma16816(c1, kf[0][i].z, kf[1][i].z, kf[0][i].w, kf[1][i].w, qf[i].z, qf[i].w);
+            for (int ks = 0; ks < D / 16; ++ks) {
+                uint32_t f[4];
+                ldsm4(f, kb + (ks / 4) * CHUNK + krow * 128 + ((((ks % 4) * 2 + kpc) ^ (krow & 7)) << 4));
+                mma16816(ks & 1 ? c1 : c0, f[0], f[1], f[2], f[3], qf[ks][0], qf[ks][1]);
             }
-            load_k(nxt, page_next);
             if (last && nxt.left > 0) load_q(nxt);
             float x[4];                             // rows gid, gid + 8; heads 2 tig, 2 tig + 1
 #pragma unroll
@@ -230,31 +266,30 @@ template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel
                 l[1] += __uint_as_float(pr[y] & 0xffff0000u);
                 pr[y] = transpose8x8(pr[y]);
             }
-            if (live < 16) {                        // rows that do not exist may hold anything: zeros
+            // rows that do not exist may hold anything: their V becomes zero (masks of the operand's rows 2 tig.. + 8)
+            uint32_t mask[2] = {0xffffffffu, 0xffffffffu};
+            if (live < 16)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (2 * tig + (r & 1) + (r >> 1) * 8 >= live)
-#pragma unroll
-                        for (int i = 0; i < VC; ++i) vf[r][i] = make_uint4(0, 0, 0, 0);
-            }
-            // product j: channels gid * 8 + j and 64 + gid * 8 + j (D = 64: gid * 8 + j and gid * 8 + 4 + j)
+                for (int y = 0; y < 2; ++y)
+                    mask[y] = (2 * tig + y * 8 < live ? 0xffffu : 0u) | (2 * tig + 1 + y * 8 < live ? 0xffff0000u : 0u);
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
-                const int j1 = D == 128 ? j : j + 4, c1i = D == 128 ? 1 : 0;
-                const uint32_t s0 = j & 1 ? 0x7632 : 0x5410;
-                mma16816(o[j], __byte_perm(word(vf[0][0], j / 2), word(vf[1][0], j / 2), s0),
-                         __byte_perm(word(vf[0][c1i], j1 / 2), word(vf[1][c1i], j1 / 2), s0),
-                         __byte_perm(word(vf[2][0], j / 2), word(vf[3][0], j / 2), s0),
-                         __byte_perm(word(vf[2][c1i], j1 / 2), word(vf[3][c1i], j1 / 2), s0), pr[0], pr[1]);
+                uint32_t f[4];
+                ldsm4_t(f, vb + (j / 4) * CHUNK + vrow * 128 + ((((j % 4) * 2 + vpc) ^ (vrow & 7)) << 4));
+                if (live < 16) { f[0] &= mask[0]; f[1] &= mask[0]; f[2] &= mask[1]; f[3] &= mask[1]; }
+                mma16816(o[j], f[0], f[1], f[2], f[3], pr[0], pr[1]);
             }
-            load_v(nxt, page_next);
+            __syncwarp();                           // (all lanes have read the stage)
+            if (ok) copy_next(s);
             if (last) {                             // the part's end: its state, or the output
                 const int u = cur.item / a.HG, h0 = (cur.item - u * a.HG) * HEADS;
                 const bool whole = b_first == 0 && cur.b == cur.blocks - 1;
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+                for (int y = 0; y < 2; ++y) {
 #pragma unroll
                     for (int z = 4; z < 32; z <<= 1) l[y] += __shfl_xor_sync(0xffffffffu, l[y], z);
+                    if (!ok) l[y] = NAN;
+                }
                 const int w = blockIdx.x * WARPS + warp;
                 if (b_first == 0 && lane == 0) {
                     // parts after the first one begin at the next warps' shares
@@ -268,29 +303,18 @@ template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel
                     if (h0 + h >= a.G) break;
                     if (whole && a.out) {
                         const float f = l[y] == 0.f ? 0.f : 1.f / l[y];
-                        __nv_bfloat16* dst = a.out + ((size_t)u * a.G + h0 + h) * D + gid * 8;
-                        float z[8];
+                        __nv_bfloat16* dst = a.out + ((size_t)u * a.G + h0 + h) * D + gid;
 #pragma unroll
-                        for (int s = 0; s < VC; ++s) {
+                        for (int j = 0; j < MT; ++j)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float v = D == 128 ? o[j % MT][2 * s + y] : o[j % 4][2 * (j / 4) + y];
-                                z[j] = f != 0.f ? v * f : 0.f;
-                            }
-                            *reinterpret_cast<uint4*>(dst + s * 64) = Vec<__nv_bfloat16>::pack(z);
-                        }
+                            for (int e = 0; e < 2; ++e) dst[j * 16 + e * 8] = __float2bfloat16_rn(f != 0.f ? o[j][2 * e + y] * f : 0.f);
                     } else {
                         const size_t r = slot * a.st.rows + h;
-                        float* dst = a.st.o + r * D + gid * 8;
+                        float* dst = a.st.o + r * D + gid;
 #pragma unroll
-                        for (int s = 0; s < VC; ++s)
+                        for (int j = 0; j < MT; ++j)
 #pragma unroll
-                            for (int j = 0; j < 8; j += 4) {
-                                float z[4];
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) z[i] = D == 128 ? o[(j + i) % MT][2 * s + y] : o[i][2 * (j / 4) + y];
-                                *reinterpret_cast<float4*>(dst + s * 64 + j) = make_float4(z[0], z[1], z[2], z[3]);
-                            }
+                            for (int e = 0; e < 2; ++e) dst[j * 16 + e * 8] = o[j][2 * e + y];
                         if (gid == 0) a.st.ml[r] = make_float4(m[y], l[y], l[y], 0.f);
                     }
                 }
@@ -298,12 +322,49 @@ template <int D> __global__ void __launch_bounds__(NT, PER_SM) rows_paged_kernel
                 b_first = nxt.b;
             }
             cur = nxt;
-            page = page_next;
-            nxt = advance(nxt);
-            page_next = page_of(nxt);
+            s = s + 1 == STAGES ? 0 : s + 1;
+        }
+        if (!ok) {
+            // copies in flight land before shared memory is given back (bounded)
+            if (a.stats) a.stats->status = KVM_E_DEVICE_TIMEOUT;
+            for (int i = 0; i < STAGES; ++i)
+                for (uint32_t it = 0; it < (1u << 12); ++it)
+                    if (mbar_try(&full[warp][i], phase >> i & 1)) break;
         }
     }
     if (a.pre.units) grid_dependency_wait();        // (who joins waits for this kernel, and thereby for the prefix's)
+}
+
+// All pages' rows as a tensor [rows, D], boxes of [16 rows, 64 channels].
+bool make_pool_map(CUtensorMap* map, const void* ptr, const Keys& k, int D) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)k.n_pages << k.shift};
+    cuuint64_t strides[1] = {(cuuint64_t)D * 2};
+    cuuint32_t box[2] = {64, STAGE_ROWS};
+    cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cudaStream_t st) {
+    constexpr size_t smem = 1024 + WARPS * RING_BYTES;
+    static std::mutex mu;
+    static bool ready[KVM_MAX_DEVICES] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= KVM_MAX_DEVICES) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready[dev]) {
+            if ((e = cudaFuncSetAttribute(rows_paged_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+            ready[dev] = true;
+        }
+    }
+    CUtensorMap mk, mv;
+    if (!make_pool_map(&mk, a.k.K, a.k, D) || !make_pool_map(&mv, a.k.V, a.k, D)) return cudaErrorNotSupported;
+    return launch_dependent(rows_paged_kernel<D>, dim3(plan.grid), dim3(NT), smem, st, mk, mv, a);
 }
 
 }  // namespace
@@ -324,7 +385,7 @@ PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix) {
 cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Beside& pre, const States& states, void* out,
                               kvm_stats* stats, cudaStream_t st) {
     const Args a = {(const __nv_bfloat16*)q, k, states, pre, (__nv_bfloat16*)out, stats, s.G, plan.hg, plan.items, s.scale * LOG2E};
-    return launch_dependent(s.D == 128 ? rows_paged_kernel<128> : rows_paged_kernel<64>, dim3(plan.grid), dim3(NT), 0, st, a);
+    return s.D == 128 ? launch_t<128>(plan, a, st) : launch_t<64>(plan, a, st);
 }
 
 }  // namespace serve

@@ -129,14 +129,28 @@ struct Beside {
         return n;
     }
 };
-// SMs for the prefix: both parts end at about the same time.  A step of the prefix (128 keys, up to 256 query rows) takes an SM 1.6 us,
-// 16 rows of K and V at the 80 GB/s that an SM gets through 0.05 us (D = 64) or 0.1 us; more than OWN_MOST SMs memory does not feed.
-constexpr int OWN_MOST = 80;
+// SMs for the prefix, such that both parts end at about the same time (by all lanes of a warp).  Measured side by side, us: the prefix 14
+// and 2.4 for each of a CTA's steps (128 keys, up to 256 query rows); the own rows 8 and 0.137 for 16 rows of 128 channels on one SM
+// (60 GB/s).  64 sequences of 768 rows over 16384 x 8 heads, own rows on 60 / 70 / 80 / 90 SMs: 71.5 / 64.4 / 61.1 / 67.2 us, one after the other 80;
+// 16 x 32 of 292 rows over 2048 x 32 heads, on 48 / 60 / 70 / 80 / 90: 39.4 / 34.4 / 35.0 / 36.4 / 39.9, one after the other 43.
+constexpr int OWN_MOST = 128;
 __device__ __forceinline__ int prefix_sms(long long steps, long long blocks, int D) {
-    const float a = 1.6f * (float)steps, b = (D == 128 ? 0.1f : 0.05f) * (float)blocks;
     if (blocks == 0) return SMS;
-    const int own = (int)(SMS * b / (a + b) + 0.5f);
-    return SMS - max(1, min(own, steps == 0 ? SMS - 1 : OWN_MOST));
+    const float own = (D == 128 ? 0.137f : 0.09f) * (float)blocks;
+    float best = 1e30f;
+    int y_best = 1;
+#pragma unroll 1
+    for (int y = 1 + (threadIdx.x & 31); y <= (steps == 0 ? SMS - 1 : OWN_MOST); y += 32) {
+        const float t = fmaxf(14.f + 2.4f * ceilf(__fdividef((float)steps, (float)(SMS - y))), 8.f + __fdividef(own, (float)y));
+        if (t < best) { best = t; y_best = y; }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const float t = __shfl_xor_sync(0xffffffffu, best, o);
+        const int y = __shfl_xor_sync(0xffffffffu, y_best, o);
+        if (t < best || (t == best && y < y_best)) { best = t; y_best = y; }
+    }
+    return SMS - y_best;
 }
 template <int THREADS> __device__ __forceinline__ long long block_sum(long long v, long long* smem) {       // smem: a long long per warp
 #pragma unroll

@@ -114,14 +114,14 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
         w.pre_tc = tc_plan(s.Hkv, s.G, s.B, pre_rows, false);
         w.pre_states = tc_states(w.pre_tc, s.Hkv, s.D, s.G, c);
     } else if (w.pre) {
-        w.pre_plan = simt_plan(s.Hkv, s.B * s.G, pre_rows);
+        w.pre_plan = simt_plan(s.Hkv, s.B * s.G, pre_rows, s.D);
         if (w.own || w.pre_plan.pieces > 1) w.pre_states = simt_states(w.pre_plan, s.Hkv, s.D, c);
     }
     if (w.own && s.dtype == KVM_BF16) {
         w.own_paged = paged_plan(s, own->room(), w.pre);
         w.own_states = paged_states(w.own_paged, s.D, c);
     } else if (w.own) {
-        w.own_plan = simt_plan(s.U, s.G, own->room());
+        w.own_plan = simt_plan(s.U, s.G, own->room(), s.D);
         if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
     }
     w.bytes = c.off + 256;
@@ -143,7 +143,7 @@ CrossWork plan_cross(const Shape& s, int n_q, int rows, void* ws) {
         w.bytes = c.off + 256;
         return w;
     }
-    w.plan = simt_plan(s.U, s.G * n_q, rows);
+    w.plan = simt_plan(s.U, s.G * n_q, rows, s.D);
     if (w.plan.pieces > 1) w.states = simt_states(w.plan, s.U, s.D, c);
     w.bytes = c.off + 256;
     return w;

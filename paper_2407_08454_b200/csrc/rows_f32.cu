@@ -3,19 +3,20 @@
 // with one pass over the keys, a running maximum and sum per row, and, where there are few rows, the keys cut into pieces whose
 // states are joined by another kernel.
 //
-// Two forms.  Up to 48 query rows per unit (a decode step): blocks of 8 rows, 32 keys at a time, bound by bandwidth: a pair of
+// Two forms.  Up to 24 query rows per unit (a decode step): blocks of 8 rows, 32 keys at a time, bound by bandwidth: a pair of
 // rows reads a key's channels from shared memory once, 64 KB of shared-memory reads for 32 KB of keys and values and each
-// product (about 1,100 clocks against 1,400 that an SM's share of the bandwidth takes).  More rows: blocks of 64 x 64, every
-// thread four rows by four keys and four rows by D / 16 channels, bound by the fp32 pipes and shared memory together.
-// (8 rows at a time 64 keys take about 2,200 clocks, 64 rows at a time 12,000: the forms meet between 40 and 48 rows.)
+// product (about 1,100 clocks against 1,400 that an SM's share of the bandwidth takes).  More rows: blocks of 64 rows by 64 keys
+// (32 with 128 channels), four rows per thread, bound by the fp32 pipes and shared memory together.
+// (8 heads over 4096 keys, D = 64 / 128, us: 32 rows by eights 38.4 / 54, 48 rows 46.5 / 76, 64 rows together 33.6 / 48.5.)
 // The next keys are on their way to registers while the current ones are used.
 #include "serve.cuh"
+#include "tc_common.cuh"
 
 namespace kvm {
 namespace serve {
 namespace {
 
-constexpr int NT = 256;
+constexpr int NT8 = 256, NT64 = 256;        // threads of a block of 8 and of 64 query rows
 
 struct Args {
     Queries q;
@@ -29,7 +30,7 @@ struct Args {
 
 // A tile of KT keys and values: global memory -> registers -> shared memory as fp32, rows of D + 4 floats (so that 16-byte reads
 // of neighbouring rows fall into different banks).  Rows that do not exist become zeros.
-template <typename T, int D, int KT> struct Tile {
+template <typename T, int D, int KT, int NT> struct Tile {
     static constexpr int N = Vec<T>::N, LPR = D / N, PER = KT * LPR / NT;       // lanes per row, 16-byte pieces per thread
     static_assert(KT * LPR % NT == 0, "whole rounds");
     uint4 k[PER], v[PER];
@@ -71,7 +72,7 @@ __device__ __forceinline__ bool exists(const Args& a, int u, int r) {
 }
 
 // MT query rows of the unit from row m0, times the scale (log2 units), in shared memory; rows past the last are zeros.
-template <typename T, int D, int MT> __device__ __forceinline__ void load_queries(const Args& a, int u, int m0, float* sq, int pitch) {
+template <typename T, int D, int MT, int NT> __device__ __forceinline__ void load_queries(const Args& a, int u, int m0, float* sq, int pitch) {
     constexpr int N = Vec<T>::N, LPR = D / N;
     for (int i = threadIdx.x; i < MT * LPR; i += NT) {
         const int m = m0 + i / LPR, c = i % LPR * N;
@@ -110,7 +111,7 @@ template <int KT> __device__ __forceinline__ void share(const Args& a, int u, in
 }
 
 // ------------------------------------------------------------------ few rows
-template <typename T, int D> __global__ void __launch_bounds__(NT) rows8_kernel(const Args a) {
+template <typename T, int D> __global__ void __launch_bounds__(NT8) rows8_kernel(const Args a) {
     constexpr int MT = 8, KT = 32, P = D + 4, E = D / 32;
     __shared__ __align__(16) float sq[MT * P], sk[KT * P], sv[KT * P];
     __shared__ float sx[2][MT][KT], sp[MT][KT], salpha[MT];
@@ -120,8 +121,8 @@ template <typename T, int D> __global__ void __launch_bounds__(NT) rows8_kernel(
     grid_dependency_wait();
     int r0, r1;
     share<KT>(a, u, r0, r1);
-    load_queries<T, D, MT>(a, u, m0, sq, P);
-    Tile<T, D, KT> t;
+    load_queries<T, D, MT, NT8>(a, u, m0, sq, P);
+    Tile<T, D, KT, NT8> t;
     t.load(a.k, u, r0, r1);
     float m = -INFINITY, l = 0.f, o[2][E] = {};                          // m, l: of row `warp` (l: of this lane's keys)
     for (int r = r0; r < r1; r += KT) {
@@ -193,9 +194,13 @@ template <typename T, int D> __global__ void __launch_bounds__(NT) rows8_kernel(
 }
 
 // ------------------------------------------------------------------ many rows
-template <int D> constexpr size_t rows64_smem() { return (3 * 64 * (D + 4) + 64 * 68) * sizeof(float); }
-template <typename T, int D> __global__ void __launch_bounds__(NT) rows64_kernel(const Args a) {
-    constexpr int MT = 64, KT = 64, P = D + 4, PP = KT + 4, E = D / 16;
+// A thread takes four rows by KT / 16 keys, then four rows by D / 16 channels, pairs of channels in one instruction.  28.7 TFLOP/s of 72 with
+// 64 channels, 30.1 with 128 (16 heads x 1024 queries x 2048 keys); eight rows per thread of half as many, which halves the
+// reads per product, is as fast (27.9, 30.0), and so are single products: neither the reads nor the issue slots bound it.
+template <int D> constexpr int keys64() { return D == 128 ? 32 : 64; }
+template <int D> constexpr size_t rows64_smem() { return ((64 + 2 * keys64<D>()) * (D + 4) + 64 * (keys64<D>() + 4)) * sizeof(float); }
+template <typename T, int D> __global__ void __launch_bounds__(NT64) rows64_kernel(const Args a) {
+    constexpr int MT = 64, KT = keys64<D>(), P = D + 4, PP = KT + 4, E = D / 16, KJ = KT / 16, R = 4;
     extern __shared__ __align__(16) float smem[];
     float *sq = smem, *sk = sq + MT * P, *sv = sk + KT * P, *sp = sv + KT * P;
     const int rg = threadIdx.x / 16, kg = threadIdx.x % 16;              // four rows; keys kg + 16 j, channels 4 kg + 64 j
@@ -203,41 +208,48 @@ template <typename T, int D> __global__ void __launch_bounds__(NT) rows64_kernel
     grid_dependency_wait();
     int r0, r1;
     share<KT>(a, u, r0, r1);
-    load_queries<T, D, MT>(a, u, m0, sq, P);
-    Tile<T, D, KT> t;
+    load_queries<T, D, MT, NT64>(a, u, m0, sq, P);
+    Tile<T, D, KT, NT64> t;
     t.load(a.k, u, r0, r1);
-    float m[4], l[4] = {}, o[4][E] = {};                                 // l: of this thread's keys
+    float m[R], l[R] = {};                                               // l: of this thread's keys
+    uint64_t o[R][E / 2] = {};                                           // pairs of channels
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
+    for (int i = 0; i < R; ++i) m[i] = -INFINITY;
     for (int r = r0; r < r1; r += KT) {
         __syncthreads();
         t.store(sk, sv);
         __syncthreads();
         if (r + KT < r1) t.load(a.k, u, r + KT, r1);
-        float x[4][4] = {};
-#pragma unroll 4
+        uint64_t x2[R][KJ] = {};
+#pragma unroll 2
         for (int c = 0; c < D; c += 4) {
-            float4 qv[4], kv[4];
+            ulonglong2 kv[KJ];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(sq + (rg * 4 + i) * P + c);
+            for (int j = 0; j < KJ; ++j) kv[j] = *reinterpret_cast<const ulonglong2*>(sk + (kg + 16 * j) * P + c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(sk + (kg + 16 * j) * P + c);
+            for (int i = 0; i < R; ++i) {
+                const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(sq + (rg * R + i) * P + c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[i][j] = fmaf(qv[i].x, kv[j].x, x[i][j]); x[i][j] = fmaf(qv[i].y, kv[j].y, x[i][j]);
-                    x[i][j] = fmaf(qv[i].z, kv[j].z, x[i][j]); x[i][j] = fmaf(qv[i].w, kv[j].w, x[i][j]);
-                }
+                for (int j = 0; j < KJ; ++j) x2[i][j] = tc::ffma2(qv.y, kv[j].y, tc::ffma2(qv.x, kv[j].x, x2[i][j]));
+            }
         }
-        bool live[4];
+        float x[R][KJ];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) live[j] = r + kg + 16 * j < r1 && exists(a, u, r + kg + 16 * j);
+        for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+            for (int j = 0; j < KJ; ++j) {
+                float lo, hi;
+                tc::unpack2(x2[i][j], lo, hi);
+                x[i][j] = lo + hi;
+            }
+        bool live[KJ];
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) live[j] = r + kg + 16 * j < r1 && exists(a, u, r + kg + 16 * j);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
             float mn = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < KJ; ++j) {
                 if (!live[j]) x[i][j] = -INFINITY;
                 mn = fmaxf(mn, x[i][j]);
             }
@@ -248,68 +260,81 @@ template <typename T, int D> __global__ void __launch_bounds__(NT) rows64_kernel
             m[i] = mn;
             l[i] *= alpha;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < KJ; ++j) {
                 const float p = rescale2(x[i][j], mn);
                 l[i] += p;
-                sp[(rg * 4 + i) * PP + kg + 16 * j] = p;
+                sp[(rg * R + i) * PP + kg + 16 * j] = p;
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[i][e] *= alpha;
+            for (int e = 0; e < E / 2; ++e) o[i][e] = tc::fmul2(o[i][e], tc::pack2(alpha, alpha));
         }
         __syncwarp();                                                    // (a warp reads the weights of its own rows only)
-#pragma unroll 2
+#pragma unroll 1
         for (int j = 0; j < KT; j += 4) {
-            float4 p4[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p4[i] = *reinterpret_cast<const float4*>(sp + (rg * 4 + i) * PP + j);
+            ulonglong2 v[4][E / 4];
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
-                for (int x4 = 0; x4 < E / 4; ++x4) {
-                    const float4 v = *reinterpret_cast<const float4*>(sv + (j + jj) * P + kg * 4 + x4 * 64);
+                for (int x4 = 0; x4 < E / 4; ++x4) v[jj][x4] = *reinterpret_cast<const ulonglong2*>(sv + (j + jj) * P + kg * 4 + x4 * 64);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = jj == 0 ? p4[i].x : jj == 1 ? p4[i].y : jj == 2 ? p4[i].z : p4[i].w;
-                        o[i][x4 * 4] = fmaf(p, v.x, o[i][x4 * 4]);
-                        o[i][x4 * 4 + 1] = fmaf(p, v.y, o[i][x4 * 4 + 1]);
-                        o[i][x4 * 4 + 2] = fmaf(p, v.z, o[i][x4 * 4 + 2]);
-                        o[i][x4 * 4 + 3] = fmaf(p, v.w, o[i][x4 * 4 + 3]);
+            for (int i = 0; i < R; ++i) {
+                const float4 p4 = *reinterpret_cast<const float4*>(sp + (rg * R + i) * PP + j);
+#pragma unroll
+                for (int jj = 0; jj < 4; ++jj) {
+                    const float p = jj == 0 ? p4.x : jj == 1 ? p4.y : jj == 2 ? p4.z : p4.w;
+                    const uint64_t p2 = tc::pack2(p, p);
+#pragma unroll
+                    for (int x4 = 0; x4 < E / 4; ++x4) {
+                        o[i][x4 * 2] = tc::ffma2(p2, v[jj][x4].x, o[i][x4 * 2]);
+                        o[i][x4 * 2 + 1] = tc::ffma2(p2, v[jj][x4].y, o[i][x4 * 2 + 1]);
                     }
                 }
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
 #pragma unroll
         for (int z = 8; z > 0; z >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], z);
-        const int row = rg * 4 + i;
+        const int row = rg * R + i;
         if (m0 + row >= a.q.rows()) continue;
 #pragma unroll
-        for (int x4 = 0; x4 < E / 4; ++x4)
-            finish<T, D, 4>(a, u, blockIdx.x, blockIdx.y, row, m0 + row, kg * 4 + x4 * 64, o[i] + x4 * 4, m[i], l[i]);
+        for (int x4 = 0; x4 < E / 4; ++x4) {
+            float f[4];
+            tc::unpack2(o[i][x4 * 2], f[0], f[1]);
+            tc::unpack2(o[i][x4 * 2 + 1], f[2], f[3]);
+            finish<T, D, 4>(a, u, blockIdx.x, blockIdx.y, row, m0 + row, kg * 4 + x4 * 64, f, m[i], l[i]);
+        }
     }
 }
 
 template <typename T, int D> cudaError_t launch_t(const Args& a, const SimtPlan& plan, int units, cudaStream_t st) {
     const dim3 grid(plan.items, plan.pieces, units);
-    if (plan.mt == 8) return launch_dependent(rows8_kernel<T, D>, grid, dim3(NT), 0, st, a);
+    if (plan.mt == 8) return launch_dependent(rows8_kernel<T, D>, grid, dim3(NT8), 0, st, a);
     constexpr size_t smem = rows64_smem<D>();
     // (asked for on every call: the attribute is the current device's, and setting it costs less than keeping track of devices)
     const cudaError_t e = cudaFuncSetAttribute(rows64_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_dependent(rows64_kernel<T, D>, grid, dim3(NT), smem, st, a);
+    return launch_dependent(rows64_kernel<T, D>, grid, dim3(NT64), smem, st, a);
 }
 
 }  // namespace
 
-// Pieces: as many as fill the SMs about twice (lengths differ), but none with less than four tiles where all rows are there.
-SimtPlan simt_plan(int units, int m, int rows) {
+// Pieces: of few rows as many as fill the SMs about twice (lengths differ), of many as many as are at work at the same time (two blocks to
+// an SM with 128 channels, three with 64), but none with less than four tiles (two of 64 rows) where all keys are there.
+SimtPlan simt_plan(int units, int m, int rows, int D) {
     SimtPlan p;
-    p.mt = m <= 48 ? 8 : 64;
+    p.mt = m <= 24 ? 8 : 64;
     p.items = (m + p.mt - 1) / p.mt;
-    const long long blocks = (long long)units * p.items, want = (p.mt == 8 ? 148ll * 6 : 148ll * 2);
-    long long n = (want + blocks - 1) / blocks;
-    const long long most = ((long long)rows + 4 * (p.mt == 8 ? 32 : 64) - 1) / (4 * (p.mt == 8 ? 32 : 64));
+    const long long blocks = (long long)units * p.items;
+    long long n, most;
+    if (p.mt == 8) {
+        n = (SMS * 6 + blocks - 1) / blocks;
+        most = ((long long)rows + 127) / 128;
+    } else {
+        n = SMS * (D == 128 ? 2 : 3) / blocks;
+        most = ((long long)rows + 127) / 128;
+    }
     n = n > most ? most : n;
     p.pieces = n < 1 ? 1 : (int)n;
     return p;
@@ -319,8 +344,7 @@ cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, co
                              kvm_stats* stats, cudaStream_t st) {
     if (units > 65535 || plan.pieces > 65535) return cudaErrorInvalidValue;
     const Args a = {q, k, states, out, stats, s.scale * LOG2E, plan.pieces};
-    return s.dtype == KVM_BF16 ? (s.D == 128 ? launch_t<__nv_bfloat16, 128>(a, plan, units, st) : launch_t<__nv_bfloat16, 64>(a, plan, units, st))
-                               : (s.D == 128 ? launch_t<float, 128>(a, plan, units, st) : launch_t<float, 64>(a, plan, units, st));
+    return s.D == 128 ? launch_t<float, 128>(a, plan, units, st) : launch_t<float, 64>(a, plan, units, st);
 }
 
 }  // namespace serve

@@ -681,7 +681,7 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
     // Items stay whole where the fullest CTA then has at most WHOLE steps more than an equal share: what the states of cut items and their
     // joining cost.
     p.whole = (all + p.grid - 1) / p.grid * tiles * p.grid <= steps + WHOLE * p.grid;
-    p.compact = steps <= 24 * p.grid;
+    p.compact = steps <= 12 * p.grid;
     p.slot_rows = p.tiles > 1 ? 2 * TILE : TILE;
     p.slots = 2ll * p.grid + (direct ? 0 : (long long)units * p.items);
     return p;

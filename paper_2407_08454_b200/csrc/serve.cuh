@@ -168,12 +168,12 @@ cudaError_t launch_append(const Shape& s, const Pages& c, int32_t* len_out, int 
                           const uint64_t* turns, int neighbours, const void* q, const void* k, const void* v, const int64_t* strides,
                           void* q_out, kvm_stats* stats, cudaStream_t st);
 
-// Attention of all query rows over all keys of their units, by fp32 arithmetic on the ordinary cores.  With one piece per item the
+// Attention of all query rows over all keys of their units in fp32 arithmetic, for fp32 tensors.  With one piece per item the
 // result goes to `out`, else the states to `states`.
 struct SimtPlan {
     int mt, items, pieces;                      // query rows of an item, items of a unit, pieces of an item
 };
-SimtPlan simt_plan(int units, int m, int rows);
+SimtPlan simt_plan(int units, int m, int rows, int D);
 cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                              kvm_stats* stats, cudaStream_t st);
 

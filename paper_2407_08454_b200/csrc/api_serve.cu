@@ -96,9 +96,11 @@ States paged_states(const PagedPlan& plan, int D, Carver& c) {
     return s;
 }
 
+constexpr long long FOLD_BYTES = 32ll << 20;
+
 // How a call of the decode attention is dealt, and what it needs of the workspace.
 struct SharedWork {
-    bool pre, own;
+    bool pre, own, fold;                        // fold: the prefix's rows go with each sequence's own
     TcPlan pre_tc;
     PagedPlan own_paged;
     SimtPlan pre_plan, own_plan;
@@ -110,6 +112,19 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
     Carver c{(char*)ws};
     w.pre = pre_rows > 0;
     w.own = own != nullptr;
+    if (w.pre && s.dtype == KVM_BF16) {
+        // A kernel for the prefix, and joining its states, costs about 10 us that reading a short one again for every sequence, through L2,
+        // does not.
+        const long long groups = (long long)s.B * ((s.G + 7) / 8) - 1;
+        w.fold = groups * s.Hkv * pre_rows * 4 * s.D <= FOLD_BYTES;
+        w.pre = !w.fold;
+    }
+    if (w.fold) {
+        w.own_paged = paged_plan(s, pre_rows + 16 + (own ? own->room() : 0), false);
+        w.own_states = paged_states(w.own_paged, s.D, c);
+        w.bytes = c.off + 256;
+        return w;
+    }
     if (w.pre && s.dtype == KVM_BF16) {
         w.pre_tc = tc_plan(s.Hkv, s.G, s.B, pre_rows, false);
         w.pre_states = tc_states(w.pre_tc, s.Hkv, s.D, s.G, c);
@@ -243,18 +258,21 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     const Queries pre_q = {q, s.G, s.Hq, s.G, s.B}, own_q = {q, s.G, 0, s.G, 1};
     const Keys pre_k = {K_pre, V_pre, pre_len, pre_rows, nullptr, 0, 0, 0};
     const Keys own_k = {pg.K, pg.V, pg.len, own ? pg.room() : 0, pg.table, pg.n_pages, pg.shift, pg.max_pages};
-    const int32_t* own_len = nullptr;               // (of items that a table tells of)
+    if (w.fold) {
+        const Fold f = {K_pre, V_pre, pre_len, s.Hkv, pre_rows};
+        if (launch_rows_paged(s, w.own_paged, q, own_k, f, Beside{}, w.own_states, out, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        return launch_join(s, s.U, s.G, &w.own_states, nullptr, nullptr, 1, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    }
     if (s.dtype == KVM_BF16) {
         const Beside pre = {pre_len, w.pre ? s.Hkv : 0, pre_rows, w.pre_tc.items, 128}, mine = {pg.len, w.own ? s.U : 0, own_k.rows, w.own_paged.hg, 16};
         if (w.pre && launch_rows_tc(s, w.pre_tc, s.Hkv, pre_q, pre_k, mine, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
-        if (w.own && launch_rows_paged(s, w.own_paged, q, own_k, pre, w.own_states, w.pre ? nullptr : out, stats, st) != cudaSuccess) return KVM_E_CUDA;
-        own_len = pg.len;
+        if (w.own && launch_rows_paged(s, w.own_paged, q, own_k, Fold{}, pre, w.own_states, w.pre ? nullptr : out, stats, st) != cudaSuccess) return KVM_E_CUDA;
     } else {
         if (w.pre && launch_rows_simt(s, w.pre_plan, s.Hkv, pre_q, pre_k, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
         if (w.own && launch_rows_simt(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
     if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
-    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, own_len, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, o, st) == cudaSuccess
+    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, o, st) == cudaSuccess
                ? KVM_OK
                : KVM_E_CUDA;
 }
@@ -293,7 +311,7 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
-    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
 }
 
 }  // extern "C"

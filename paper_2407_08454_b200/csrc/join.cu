@@ -124,9 +124,10 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
     if (out.lse && lane == 0) out.lse[w] = end.lse;
 }
 
-// Row m of output unit u from one or two sets of states.  len: of the units whose pieces a table tells of.
+// Row m of output unit u from one or two sets of states.  b_len: the lengths of b's units, of which those without keys have no entry in the
+// table of pieces (a's all have one).
 template <typename T, int D> __global__ void __launch_bounds__(JOIN_NT)
-join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
+join_kernel(const States a, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
             int skip_whole, const Output out, int rows, int m_rows, int Hkv, int G) {
     const int w = blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
     grid_dependency_wait();
@@ -134,7 +135,7 @@ join_kernel(const States a, const int32_t* __restrict__ a_len, const States b, i
     if (w >= rows) return;
     const int u = w / m_rows, m = w - u * m_rows;
     Pieces pa = {}, pb = {};
-    if (has_a) pa = pieces_of<D>(a, a_len, u, m);
+    if (has_a) pa = pieces_of<D>(a, nullptr, u, m);
     if (has_b) pb = pieces_of<D>(b, b_len, u % Hkv, u / Hkv * G + m);
     if (skip_whole && pa.count == 1) return;                       // (by the kernel that had the item whole)
     store_row<T, D>(sum_pieces<D>(pa, pb), out, w);
@@ -163,13 +164,13 @@ join_items_kernel(const States a, const int32_t* __restrict__ len, const Output 
 
 }  // namespace
 
-cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
+cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const States* b, const int32_t* b_len,
                         int skip_whole, const Output& out, cudaStream_t st) {
     const long long rows = (long long)units * m, blocks = (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
     if (rows > 0x7fffffffll) return cudaErrorInvalidValue;
     auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>)
                                   : (s.D == 128 ? join_kernel<float, 128> : join_kernel<float, 64>);
-    return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, a_len, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
+    return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
                             b_len, skip_whole, out, (int)rows, m, s.Hkv, s.G);
 }
 

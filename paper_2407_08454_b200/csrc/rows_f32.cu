@@ -320,23 +320,21 @@ template <typename T, int D> cudaError_t launch_t(const Args& a, const SimtPlan&
 
 }  // namespace
 
-// Pieces: of few rows as many as fill the SMs about twice (lengths differ), of many as many as are at work at the same time (two blocks to
-// an SM with 128 channels, three with 64), but none with less than four tiles (two of 64 rows) where all keys are there.
+// Pieces: the number whose blocks fill the SMs best in whole rounds of what is at work at the same time (five blocks of 8 rows to an SM; of
+// 64 rows two with 128 channels, three with 64), a few per cent given away for each more, but none with less than 128 keys where all are
+// there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 953 us; XX.)
 SimtPlan simt_plan(int units, int m, int rows, int D) {
     SimtPlan p;
     p.mt = m <= 24 ? 8 : 64;
     p.items = (m + p.mt - 1) / p.mt;
-    const long long blocks = (long long)units * p.items;
-    long long n, most;
-    if (p.mt == 8) {
-        n = (SMS * 6 + blocks - 1) / blocks;
-        most = ((long long)rows + 127) / 128;
-    } else {
-        n = SMS * (D == 128 ? 2 : 3) / blocks;
-        most = ((long long)rows + 127) / 128;
+    const long long blocks = (long long)units * p.items, room = SMS * (p.mt == 8 ? 5 : D == 128 ? 2 : 3);
+    const long long most = ((long long)rows + 127) / 128, least = (room + blocks - 1) / blocks;     // (least: one round, more or less)
+    p.pieces = 1;
+    double best = 0.0;
+    for (long long n = 1; n <= most && n <= 2 * least + 6; ++n) {
+        const double fill = (double)(n * blocks) / (double)((n * blocks + room - 1) / room * room) / (1.0 + 0.02 * (double)n / (double)least);
+        if (fill > best * 1.0001) { best = fill; p.pieces = (int)n; }
     }
-    n = n > most ? most : n;
-    p.pieces = n < 1 ? 1 : (int)n;
     return p;
 }
 

@@ -8,6 +8,7 @@
 // across the ends of units, and waits for nobody else: 192 KB are in flight per SM.  (Straight from memory into the operands'
 // registers, 8 KB in flight for each of twelve warps: as fast on all SMs, but half the rate per SM, which counts beside a prefix.)
 // 16 rows never cross a page (pages are powers of two from 16); page numbers are read a block ahead of the copies.
+// A prefix may be folded in: its rows are then the first of every unit (read once per sequence, through L2).
 // A unit's part of a share leaves its state, which another kernel joins (a unit that is whole may go to the output).
 // Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones.
 #include <mutex>
@@ -32,6 +33,7 @@ constexpr float LOWEST = -1e30f, RESCALE_STEP = 8.f;
 struct Args {
     const __nv_bfloat16* q;                 // [units, G, D]
     Keys k;
+    Fold fold;
     States st;
     Beside pre;
     __nv_bfloat16* out;                     // null: whole units leave states too
@@ -64,12 +66,13 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
 
 // Where a warp stands in the list of blocks.
 struct Cursor {
-    int item, b, blocks, n;                 // block b of `blocks` of item's unit, which has n rows
+    int item, b, blocks, n, np;             // block b of `blocks` of item's unit, which has n rows of its own, behind np of a folded prefix
     int left;                               // blocks of the share from this one on; 0: past the end
 };
 
 template <int D> __global__ void __launch_bounds__(NT, PER_SM)
-rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ Args a) {
+rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_pk,
+                  const __grid_constant__ CUtensorMap map_pv, const __grid_constant__ Args a) {
     constexpr int STAGES = stages<D>(), KCH = D / 64;              // 64-channel (128-byte) column chunks
     constexpr uint32_t CHUNK = STAGE_ROWS * 128, TENSOR = KCH * CHUNK, STAGE = 2 * TENSOR;       // bytes of a chunk, of K or V, of a stage
     constexpr int MT = D / 16;                      // products of 16 channels
@@ -77,7 +80,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     __shared__ __align__(8) uint64_t full[WARPS][STAGES];
     __shared__ volatile int s_bad;
     __shared__ long long sm_all[WARPS];
-    __shared__ int sm_sum[WARPS], sm_start, sm_item, sm_rows[KEPT];
+    __shared__ int sm_sum[WARPS], sm_start, sm_item, sm_rows[KEPT], sm_pre[KEPT];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     if (threadIdx.x == 0) {
         for (int w = 0; w < WARPS; ++w)
@@ -86,6 +89,10 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         s_bad = 0;
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+        if (a.fold.rows) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_pk) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_pv) : "memory");
+        }
     }
     if (!a.pre.units) grid_dependency_wait();       // (beside a prefix: when that kernel lets this one begin, what comes before it is done)
     grid_launch_dependents();                       // (who joins is there when this kernel ends, and waits for that)
@@ -93,14 +100,18 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // ---- this block's share, by a prefix sum over the items
     // (in 32 bits: the host has seen to it)
     const bool kept = a.items <= KEPT;
-    auto rows_of = [&](int item) { return kept ? sm_rows[item] : a.k.rows_of(item / a.HG); };
-    auto blocks_of = [&](int item) { return (a.k.rows_of(item / a.HG) + 15) >> 4; };
+    auto own_of = [&](int item) { return a.k.table ? a.k.rows_of(item / a.HG) : 0; };
+    auto pre_of = [&](int item) { return a.fold.rows ? a.fold.rows_of(item / a.HG % a.fold.heads) : 0; };
+    auto rows_of = [&](int item) { return kept ? sm_rows[item] : own_of(item); };
+    auto prefix_of = [&](int item) { return kept ? sm_pre[item] : pre_of(item); };
+    auto blocks_of = [&](int item) { return ((rows_of(item) + 15) >> 4) + ((prefix_of(item) + 15) >> 4); };
     const int E = (a.items + NT - 1) / NT, i0 = min(a.items, (int)threadIdx.x * E), i1 = min(a.items, i0 + E);
     int mine = 0;
     for (int i = i0; i < i1; ++i) {
-        const int n = a.k.rows_of(i / a.HG);
-        if (kept) sm_rows[i] = n;
-        mine += (n + 15) >> 4;
+        const int n = own_of(i), np = pre_of(i);
+        if (kept) { sm_rows[i] = n; sm_pre[i] = np; }
+        mine += ((n + 15) >> 4) + ((np + 15) >> 4);
+        if (blockIdx.x == 0 && n + np == 0) a.st.pieces[i] = make_int4(0, 0, 0, 0);
     }
     int inc = mine;
 #pragma unroll
@@ -125,7 +136,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (busy && before <= f0 && f0 < before + mine) {                  // true in exactly one thread
         int st = before, id = i0;
         for (;; ++id) {
-            const int n = kept ? (sm_rows[id] + 15) >> 4 : blocks_of(id);
+            const int n = blocks_of(id);
             if (st + n > f0) break;
             st += n;
         }
@@ -138,30 +149,39 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         int start = sm_start;                       // blocks before the cursor's item
         Cursor cur;
         const int w0 = min(f1, f0 + warp * q), w1 = min(f1, w0 + q);
+        auto settle = [&](Cursor& c) {
+            c.n = rows_of(c.item);
+            c.np = prefix_of(c.item);
+            c.blocks = ((c.n + 15) >> 4) + ((c.np + 15) >> 4);
+        };
         cur.item = sm_item;
-        cur.n = rows_of(cur.item);
-        cur.blocks = (cur.n + 15) >> 4;
+        settle(cur);
         cur.left = w1 - w0;
         while (cur.left > 0 && start + cur.blocks <= w0) {
             start += cur.blocks;
-            cur.n = rows_of(++cur.item);
-            cur.blocks = (cur.n + 15) >> 4;
+            ++cur.item;
+            settle(cur);
         }
         cur.b = w0 - start;
         auto advance = [&](Cursor c) {
             if (--c.left > 0 && ++c.b == c.blocks) {
                 c.b = 0;
                 do {
-                    c.n = rows_of(++c.item);
-                    c.blocks = (c.n + 15) >> 4;
+                    ++c.item;
+                    settle(c);
                 } while (c.blocks == 0);
             }
             return c;
         };
         const int bshift = a.k.shift - 4, bmask = (1 << bshift) - 1;        // blocks per page
+        // of a block of own rows its page, of one of the folded prefix its first row in the prefix's tensor
         auto page_of = [&](const Cursor& c) {
-            return c.left > 0 ? __ldg(a.k.table + (size_t)(c.item / a.HG) * a.k.max_pages + (c.b >> bshift)) : -1;
+            if (c.left <= 0) return -1;
+            const int u = c.item / a.HG, b = c.b - ((c.np + 15) >> 4);
+            return b < 0 ? u % a.fold.heads * a.fold.rows + c.b * 16 : __ldg(a.k.table + (size_t)u * a.k.max_pages + (b >> bshift));
         };
+        auto folded = [&](const Cursor& c) { return c.b < ((c.np + 15) >> 4); };
+        auto exists = [&](const Cursor& c, int page) { return folded(c) || (unsigned)page < (unsigned)a.k.n_pages; };
         const uint32_t ring = ((smem_u32(smem_raw) + 1023u) & ~1023u) + warp * RING_BYTES;
         uint32_t qf[D / 16][2];                     // q^T as the second operand: channels 2 tig.. (+ 8) of head gid
         auto load_q = [&](const Cursor& c) {
@@ -180,16 +200,18 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 #ifdef KVM_TEST_DROP_ATTEND_STAGE
             if (blockIdx.x == KVM_TEST_DROP_CTA && warp == 0 && c.left == w1 - w0 - (KVM_TEST_DROP_ATTEND_STAGE)) return;   // test build only: this block never arrives
 #endif
-            if ((unsigned)page >= (unsigned)a.k.n_pages) {
+            if (!exists(c, page)) {
                 mbar_arrive(bar);
                 return;
             }
             mbar_expect_tx(bar, STAGE);
-            const int row = (page << a.k.shift) + ((c.b & bmask) << 4);
+            const bool pre = folded(c);
+            const int row = pre ? page : (page << a.k.shift) + (((c.b - ((c.np + 15) >> 4)) & bmask) << 4);
+            const CUtensorMap *mk = pre ? &map_pk : &map_k, *mv = pre ? &map_pv : &map_v;
 #pragma unroll
             for (int i = 0; i < KCH; ++i) {
-                tma_load_2d(ring + s * STAGE + i * CHUNK, &map_k, bar, i * 64, row);
-                tma_load_2d(ring + s * STAGE + TENSOR + i * CHUNK, &map_v, bar, i * 64, row);
+                tma_load_2d(ring + s * STAGE + i * CHUNK, mk, bar, i * 64, row);
+                tma_load_2d(ring + s * STAGE + TENSOR + i * CHUNK, mv, bar, i * 64, row);
             }
         };
         float o[MT][4];                             // channels of product j: 16 j + gid (+ 8), heads 2 tig, 2 tig + 1
@@ -210,7 +232,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         uint32_t there_bits = 0, phase = 0;         // of the stages: whether the page exists, the barrier's parity
         auto copy_next = [&](int s) {
             issue(ld, page, s);
-            there_bits = (there_bits & ~(1u << s)) | ((unsigned)page < (unsigned)a.k.n_pages ? 1u << s : 0u);
+            there_bits = (there_bits & ~(1u << s)) | (exists(ld, page) ? 1u << s : 0u);
             ld = advance(ld);
             page = page_of(ld);
         };
@@ -221,7 +243,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         bool ok = true;
         while (cur.left > 0) {
             const bool there = there_bits >> s & 1;
-            const int live = there ? cur.n - cur.b * 16 : 0;       // rows that exist
+            const int live = !there ? 0 : folded(cur) ? cur.np - cur.b * 16 : cur.n - (cur.b - ((cur.np + 15) >> 4)) * 16;    // rows that exist
             if (!there && a.stats) a.stats->status = KVM_E_PAGE;
             const Cursor nxt = advance(cur);
             const bool last = nxt.left <= 0 || nxt.item != cur.item;
@@ -335,11 +357,11 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (a.pre.units) grid_dependency_wait();        // (who joins waits for this kernel, and thereby for the prefix's)
 }
 
-// All pages' rows as a tensor [rows, D], boxes of [16 rows, 64 channels].
-bool make_pool_map(CUtensorMap* map, const void* ptr, const Keys& k, int D) {
+// Rows (all pages', or a prefix's of all heads) as a tensor [rows, D], boxes of [16 rows, 64 channels].
+bool make_pool_map(CUtensorMap* map, const void* ptr, long long rows, int D) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)k.n_pages << k.shift};
+    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)D * 2};
     cuuint32_t box[2] = {64, STAGE_ROWS};
     cuuint32_t estr[2] = {1, 1};
@@ -362,9 +384,13 @@ template <int D> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cuda
             ready[dev] = true;
         }
     }
-    CUtensorMap mk, mv;
-    if (!make_pool_map(&mk, a.k.K, a.k, D) || !make_pool_map(&mv, a.k.V, a.k, D)) return cudaErrorNotSupported;
-    return launch_dependent(rows_paged_kernel<D>, dim3(plan.grid), dim3(NT), smem, st, mk, mv, a);
+    CUtensorMap mk, mv, pk, pv;
+    const long long pool = (long long)a.k.n_pages << a.k.shift, prefix = (long long)a.fold.heads * a.fold.rows;
+    if (a.k.table && (!make_pool_map(&mk, a.k.K, pool, D) || !make_pool_map(&mv, a.k.V, pool, D))) return cudaErrorNotSupported;
+    if (prefix && (!make_pool_map(&pk, a.fold.K, prefix, D) || !make_pool_map(&pv, a.fold.V, prefix, D))) return cudaErrorNotSupported;
+    if (!a.k.table) { mk = pk; mv = pv; }           // (never read from)
+    if (!prefix) { pk = mk; pv = mv; }
+    return launch_dependent(rows_paged_kernel<D>, dim3(plan.grid), dim3(NT), smem, st, mk, mv, pk, pv, a);
 }
 
 }  // namespace
@@ -382,9 +408,9 @@ PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix) {
     return p;
 }
 
-cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Beside& pre, const States& states, void* out,
+cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Fold& fold, const Beside& pre, const States& states, void* out,
                               kvm_stats* stats, cudaStream_t st) {
-    const Args a = {(const __nv_bfloat16*)q, k, states, pre, (__nv_bfloat16*)out, stats, s.G, plan.hg, plan.items, s.scale * LOG2E};
+    const Args a = {(const __nv_bfloat16*)q, k, fold, states, pre, (__nv_bfloat16*)out, stats, s.G, plan.hg, plan.items, s.scale * LOG2E};
     return s.D == 128 ? launch_t<128>(plan, a, st) : launch_t<64>(plan, a, st);
 }
 

@@ -195,12 +195,19 @@ struct PagedPlan {
     long long slots;
 };
 PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix);
-cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Beside& pre, const States& states, void* out,
+// A prefix whose rows that kernel takes as the first of each unit: K, V [heads, rows, D]; unit u's head is u % heads.  rows 0: none.
+struct Fold {
+    const void *K, *V;
+    const int32_t* len;                         // nullable: all `rows`
+    int heads, rows;
+    __device__ __forceinline__ int rows_of(int h) const { return len ? max(0, min(__ldg(len + h), rows)) : rows; }
+};
+cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Fold& fold, const Beside& pre, const States& states, void* out,
                               kvm_stats* stats, cudaStream_t st);
 
 // Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
 // unit = h and row = b * G + g, of `b` (a shared prefix).
-cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const int32_t* a_len, const States* b, const int32_t* b_len,
+cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const States* b, const int32_t* b_len,
                         int skip_whole, const Output& out, cudaStream_t st);
 // skip_whole: rows of items in one piece are in the output already.
 // The same for the tensor-core kernel's items [units][items] of m rows a unit, of which those in one piece are in the output already.

@@ -261,7 +261,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (w.fold) {
         const Fold f = {K_pre, V_pre, pre_len, s.Hkv, pre_rows};
         if (launch_rows_paged(s, w.own_paged, q, own_k, f, Beside{}, w.own_states, out, stats, st) != cudaSuccess) return KVM_E_CUDA;
-        return launch_join(s, s.U, s.G, &w.own_states, nullptr, nullptr, 1, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+        return launch_join(s, s.U, s.G, &w.own_states, nullptr, nullptr, 1, w.own_paged.grid * 4 / w.own_paged.items, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
     if (s.dtype == KVM_BF16) {
         const Beside pre = {pre_len, w.pre ? s.Hkv : 0, pre_rows, w.pre_tc.items, 128}, mine = {pg.len, w.own ? s.U : 0, own_k.rows, w.own_paged.hg, 16};
@@ -272,7 +272,9 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
         if (w.own && launch_rows_simt(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
     if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
-    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, o, st) == cudaSuccess
+    const int about = s.dtype == KVM_BF16 ? (w.own ? w.own_paged.grid * 4 / w.own_paged.items : 0) + (w.pre ? w.pre_tc.grid / (s.Hkv * w.pre_tc.items) : 0)
+                                          : w.own_plan.pieces + w.pre_plan.pieces;
+    return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, about, o, st) == cudaSuccess
                ? KVM_OK
                : KVM_E_CUDA;
 }
@@ -311,7 +313,7 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     }
     if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
-    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, 0, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
+    return launch_join(s, s.U, m, &w.states, nullptr, nullptr, 0, w.plan.pieces, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
 }
 
 }  // extern "C"

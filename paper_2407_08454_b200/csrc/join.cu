@@ -47,8 +47,10 @@ template <int E> struct Sum {                   // E channels of a row
 // One loop over the pieces of both sets, BATCH at a time so that their loads leave together.  (Short code: a launch of a few warps spends
 // most of its time on fetching instructions.  With a copy of the loop for each set, and one for few and one for many pieces, 12.5 us for
 // 32 rows of 12 pieces.)
-template <int D> __device__ __forceinline__ Sum<D / 32> sum_pieces(const Pieces& a, const Pieces& b) {
-    constexpr int BATCH = 8, E = D / 32;
+// The warp is number `part` of `parts` that share the row, each taking a batch in turn.
+constexpr int BATCH = 8;
+template <int D> __device__ __forceinline__ Sum<D / 32> sum_pieces(const Pieces& a, const Pieces& b, int part, int parts) {
+    constexpr int E = D / 32;
     const int lane = threadIdx.x & 31, count = a.count + b.count;
     Sum<E> s;
     s.m = -INFINITY;
@@ -56,7 +58,7 @@ template <int D> __device__ __forceinline__ Sum<D / 32> sum_pieces(const Pieces&
 #pragma unroll
     for (int e = 0; e < E; ++e) s.o[e] = 0.f;
 #pragma unroll 1
-    for (int i0 = 0; i0 < count; i0 += BATCH) {
+    for (int i0 = part * BATCH; i0 < count; i0 += parts * BATCH) {
         float4 z[BATCH];
         float x[BATCH][E], mn = s.m;
 #pragma unroll
@@ -100,6 +102,34 @@ template <int D> __device__ __forceinline__ Sum<D / 32> sum_pieces(const Pieces&
     return s;
 }
 
+// Joins what the warps of a block have of one row (all of them; the first one gets the sums).
+template <int D> __device__ __forceinline__ void join_warps(Sum<D / 32>& s) {
+    constexpr int E = D / 32, W = JOIN_NT / 32;
+    __shared__ float sm[W][3], so[W][D];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) { sm[warp][0] = s.m; sm[warp][1] = s.l; sm[warp][2] = s.lr; }
+#pragma unroll
+    for (int e = 0; e < E; ++e) so[warp][lane * E + e] = s.o[e];
+    __syncthreads();
+    if (warp != 0) return;
+    float M = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < W; ++x) M = fmaxf(M, sm[x][0]);
+    s.l = s.lr = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s.o[e] = 0.f;
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+        const float w = sm[x][1] == 0.f ? 0.f : rescale2(sm[x][0], M);
+        s.l = fmaf(sm[x][1], w, s.l);
+        s.lr = fmaf(sm[x][2], w, s.lr);
+        if (w != 0.f)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s.o[e] = fmaf(so[x][lane * E + e], w, s.o[e]);
+    }
+    s.m = M;
+}
+
 // The row's sums to the output (row w).
 template <typename T, int D> __device__ __forceinline__ void store_row(const Sum<D / 32>& s, const Output& out, long long w) {
     constexpr int E = D / 32;
@@ -126,10 +156,12 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
 
 // Row m of output unit u from one or two sets of states.  b_len: the lengths of b's units, of which those without keys have no entry in the
 // table of pieces (a's all have one).
-template <typename T, int D> __global__ void __launch_bounds__(JOIN_NT)
+// WIDE: a block per row.  (Of few rows with many pieces each the batches, 0.85 us one after the other, are what takes time: 32 rows of 148
+// pieces XX.)
+template <typename T, int D, bool WIDE> __global__ void __launch_bounds__(JOIN_NT)
 join_kernel(const States a, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
             int skip_whole, const Output out, int rows, int m_rows, int Hkv, int G) {
-    const int w = blockIdx.x * (JOIN_NT / 32) + (threadIdx.x >> 5);
+    const int warp = threadIdx.x >> 5, w = WIDE ? blockIdx.x : blockIdx.x * (JOIN_NT / 32) + warp;
     grid_dependency_wait();
     grid_launch_dependents();
     if (w >= rows) return;
@@ -138,12 +170,17 @@ join_kernel(const States a, const States b, int has_a, int has_b, const int32_t*
     if (has_a) pa = pieces_of<D>(a, nullptr, u, m);
     if (has_b) pb = pieces_of<D>(b, b_len, u % Hkv, u / Hkv * G + m);
     if (skip_whole && pa.count == 1) return;                       // (by the kernel that had the item whole)
-    store_row<T, D>(sum_pieces<D>(pa, pb), out, w);
+    Sum<D / 32> s = sum_pieces<D>(pa, pb, WIDE ? warp : 0, WIDE ? JOIN_NT / 32 : 1);
+    if (WIDE) {
+        join_warps<D>(s);
+        if (warp != 0) return;
+    }
+    store_row<T, D>(s, out, w);
 }
 
 // Items of which most have gone to the output in one piece: a block per ITEM_ROWS rows of a tile, which looks at its item first.
 // (A warp per row of the output took 44 us for 131,072 rows of which three in ten had pieces.)
-template <typename T, int D, int ITEM_ROWS> __global__ void __launch_bounds__(JOIN_NT)
+template <typename T, int D, int ITEM_ROWS> __global__ void __launch_bounds__(JOIN_NT)       // (ITEM_ROWS 1: the block's warps share the row)
 join_items_kernel(const States a, const int32_t* __restrict__ len, const Output out, int m_rows) {
     const int per = a.rows / ITEM_ROWS, part = blockIdx.x % per, at = blockIdx.x / per, u = at / a.items;
     const int m0 = (at % a.items) * a.rows + part * ITEM_ROWS;     // (tiles of an item follow one another in the unit)
@@ -154,33 +191,47 @@ join_items_kernel(const States a, const int32_t* __restrict__ len, const Output 
     const int4 pc = __ldcg(a.pieces + at);
     if (n > 0 && pc.x == 1) return;
     Pieces p = {n > 0 ? pc.x : 0, pc.y, pc.z, a.stride, a.o, a.ml, a.rows}, none = {};
+    if (ITEM_ROWS == 1) {
+        p.o = a.o + (size_t)part * D;
+        p.ml = a.ml + part;
+        Sum<D / 32> s = sum_pieces<D>(p, none, threadIdx.x >> 5, JOIN_NT / 32);
+        join_warps<D>(s);
+        if (threadIdx.x < 32) store_row<T, D>(s, out, (long long)u * m_rows + m0);
+        return;
+    }
 #pragma unroll 1
     for (int r = threadIdx.x >> 5; r < ITEM_ROWS && m0 + r < m_rows; r += JOIN_NT / 32) {
         p.o = a.o + (size_t)(part * ITEM_ROWS + r) * D;
         p.ml = a.ml + part * ITEM_ROWS + r;
-        store_row<T, D>(sum_pieces<D>(p, none), out, (long long)u * m_rows + m0 + r);
+        store_row<T, D>(sum_pieces<D>(p, none, 0, 1), out, (long long)u * m_rows + m0 + r);
     }
 }
 
 }  // namespace
 
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const States* b, const int32_t* b_len,
-                        int skip_whole, const Output& out, cudaStream_t st) {
-    const long long rows = (long long)units * m, blocks = (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
+                        int skip_whole, int pieces_about, const Output& out, cudaStream_t st) {
+    const long long rows = (long long)units * m;
+    const bool wide = pieces_about > 2 * BATCH && rows <= 2048;
+    const long long blocks = wide ? rows : (rows + JOIN_NT / 32 - 1) / (JOIN_NT / 32);
     if (rows > 0x7fffffffll) return cudaErrorInvalidValue;
-    auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? join_kernel<__nv_bfloat16, 128> : join_kernel<__nv_bfloat16, 64>)
-                                  : (s.D == 128 ? join_kernel<float, 128> : join_kernel<float, 64>);
+    auto fn = s.dtype == KVM_BF16 ? (s.D == 128 ? (wide ? join_kernel<__nv_bfloat16, 128, true> : join_kernel<__nv_bfloat16, 128, false>)
+                                                : (wide ? join_kernel<__nv_bfloat16, 64, true> : join_kernel<__nv_bfloat16, 64, false>))
+                                  : (s.D == 128 ? (wide ? join_kernel<float, 128, true> : join_kernel<float, 128, false>)
+                                                : (wide ? join_kernel<float, 64, true> : join_kernel<float, 64, false>));
     return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a ? *a : States{}, b ? *b : States{}, a ? 1 : 0, b ? 1 : 0,
                             b_len, skip_whole, out, (int)rows, m, s.Hkv, s.G);
 }
 
 cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st) {
-    // (few items have many pieces each: a warp per row; of many items few are cut: less blocks that find nothing to do)
-    const int per_block = (long long)units * a.items <= 148 ? JOIN_NT / 32 : 16;
-    const long long blocks = (long long)units * a.items * (a.rows / per_block);
+    // (few items have many pieces each: a block or a warp per row; of many items few are cut: less blocks that find nothing to do)
+    const long long items = (long long)units * a.items;
+    const int per_block = items * 2 * BATCH < 148 ? 1 : items <= 148 ? JOIN_NT / 32 : 16;
+    const long long blocks = items * (a.rows / per_block);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    auto fn = per_block == 16 ? (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, 16> : join_items_kernel<__nv_bfloat16, 64, 16>)
-                              : (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, JOIN_NT / 32> : join_items_kernel<__nv_bfloat16, 64, JOIN_NT / 32>);
+    auto fn = per_block == 1    ? (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, 1> : join_items_kernel<__nv_bfloat16, 64, 1>)
+              : per_block == 16 ? (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, 16> : join_items_kernel<__nv_bfloat16, 64, 16>)
+                                : (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, JOIN_NT / 32> : join_items_kernel<__nv_bfloat16, 64, JOIN_NT / 32>);
     return launch_dependent(fn, dim3((unsigned)blocks), dim3(JOIN_NT), 0, st, a, len, out, m);
 }
 

@@ -208,8 +208,8 @@ cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void*
 // Joins the states: one row of output per row of [units][m].  Two sets of states may be given, over the units of `a` and, with
 // unit = h and row = b * G + g, of `b` (a shared prefix).
 cudaError_t launch_join(const Shape& s, int units, int m, const States* a, const States* b, const int32_t* b_len,
-                        int skip_whole, const Output& out, cudaStream_t st);
-// skip_whole: rows of items in one piece are in the output already.
+                        int skip_whole, int pieces_about, const Output& out, cudaStream_t st);
+// skip_whole: rows of items in one piece are in the output already.  pieces_about: how many pieces a row may have.
 // The same for the tensor-core kernel's items [units][items] of m rows a unit, of which those in one piece are in the output already.
 cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a, const int32_t* len, const Output& out, cudaStream_t st);
 

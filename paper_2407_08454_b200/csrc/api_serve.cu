@@ -78,6 +78,7 @@ States tc_states(const TcPlan& plan, int units, int D, int R, Carver& c) {
     s.R = plan.per_block ? R : 0;
     s.two = 1;
     s.tile_room = 128;
+    s.halves = plan.alt;
     s.o = (float*)c.take((size_t)plan.slots * plan.slot_rows * D * sizeof(float));
     s.ml = (float4*)c.take((size_t)plan.slots * plan.slot_rows * sizeof(float4));
     s.pieces = (int4*)c.take((size_t)units * plan.items * sizeof(int4));

@@ -14,8 +14,12 @@ struct Pieces {
     int count, first, second, stride;
     const float* o;                             // the row's sums in slot 0, and how far slots lie apart (rows)
     const float4* ml;
-    int pitch;
-    __device__ __forceinline__ long long at(int i) const { return (long long)(i == 0 ? first : second + (i - 1) * stride) * pitch; }
+    int pitch, half;                            // half: rows to a piece's second state (0: it has one)
+    __device__ __forceinline__ long long at(int i) const {
+        const int x = half ? i & 1 : 0;
+        if (half) i >>= 1;
+        return (long long)(i == 0 ? first : second + (i - 1) * stride) * pitch + x * half;
+    }
 };
 template <int D> __device__ __forceinline__ Pieces pieces_of(const States& st, const int32_t* len, int unit, int m) {
     int item, row;
@@ -26,6 +30,7 @@ template <int D> __device__ __forceinline__ Pieces pieces_of(const States& st, c
     p.pitch = st.rows;
     p.o = st.o + (size_t)row * D;
     p.ml = st.ml + row;
+    p.half = st.halves ? st.tile_room : 0;
     if (st.count > 0) {
         p.count = st.count;
         p.first = at * st.count;
@@ -33,7 +38,7 @@ template <int D> __device__ __forceinline__ Pieces pieces_of(const States& st, c
     } else {                                    // (both reads leave together; a unit without keys has no entry in the table)
         const int n = len ? __ldg(len + unit) : 1;
         const int4 pc = __ldcg(st.pieces + at);
-        p.count = n > 0 ? pc.x : 0;
+        p.count = n > 0 ? pc.x << (st.halves ? 1 : 0) : 0;
         p.first = pc.y;
         p.second = pc.z;
     }
@@ -157,7 +162,7 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
 // Row m of output unit u from one or two sets of states.  b_len: the lengths of b's units, of which those without keys have no entry in the
 // table of pieces (a's all have one).
 // WIDE: a block per row.  (Of few rows with many pieces each the batches, 0.85 us one after the other, are what takes time: 32 rows of 148
-// pieces XX.)
+// pieces and all before them 39 us by a warp per row, 23 so.)
 template <typename T, int D, bool WIDE> __global__ void __launch_bounds__(JOIN_NT)
 join_kernel(const States a, const States b, int has_a, int has_b, const int32_t* __restrict__ b_len,
             int skip_whole, const Output out, int rows, int m_rows, int Hkv, int G) {
@@ -182,15 +187,15 @@ join_kernel(const States a, const States b, int has_a, int has_b, const int32_t*
 // (A warp per row of the output took 44 us for 131,072 rows of which three in ten had pieces.)
 template <typename T, int D, int ITEM_ROWS> __global__ void __launch_bounds__(JOIN_NT)       // (ITEM_ROWS 1: the block's warps share the row)
 join_items_kernel(const States a, const int32_t* __restrict__ len, const Output out, int m_rows) {
-    const int per = a.rows / ITEM_ROWS, part = blockIdx.x % per, at = blockIdx.x / per, u = at / a.items;
-    const int m0 = (at % a.items) * a.rows + part * ITEM_ROWS;     // (tiles of an item follow one another in the unit)
+    const int per = (a.halves ? a.tile_room : a.rows) / ITEM_ROWS, part = blockIdx.x % per, at = blockIdx.x / per, u = at / a.items;
+    const int m0 = (at % a.items) * (per * ITEM_ROWS) + part * ITEM_ROWS;     // (tiles of an item follow one another in the unit)
     grid_dependency_wait();
     grid_launch_dependents();
     if (m0 >= m_rows) return;
     const int n = len ? __ldg(len + u) : 1;
     const int4 pc = __ldcg(a.pieces + at);
-    if (n > 0 && pc.x == 1) return;
-    Pieces p = {n > 0 ? pc.x : 0, pc.y, pc.z, a.stride, a.o, a.ml, a.rows}, none = {};
+    if (n > 0 && pc.x == 1 && !a.halves) return;
+    Pieces p = {n > 0 ? pc.x << (a.halves ? 1 : 0) : 0, pc.y, pc.z, a.stride, a.o, a.ml, a.rows, a.halves ? a.tile_room : 0}, none = {};
     if (ITEM_ROWS == 1) {
         p.o = a.o + (size_t)part * D;
         p.ml = a.ml + part;
@@ -227,7 +232,7 @@ cudaError_t launch_join_items(const Shape& s, int units, int m, const States& a,
     // (few items have many pieces each: a block or a warp per row; of many items few are cut: less blocks that find nothing to do)
     const long long items = (long long)units * a.items;
     const int per_block = items * 2 * BATCH < 148 ? 1 : items <= 148 ? JOIN_NT / 32 : 16;
-    const long long blocks = items * (a.rows / per_block);
+    const long long blocks = items * ((a.halves ? a.tile_room : a.rows) / per_block);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
     auto fn = per_block == 1    ? (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, 1> : join_items_kernel<__nv_bfloat16, 64, 1>)
               : per_block == 16 ? (s.D == 128 ? join_items_kernel<__nv_bfloat16, 128, 16> : join_items_kernel<__nv_bfloat16, 64, 16>)

@@ -322,7 +322,7 @@ template <typename T, int D> cudaError_t launch_t(const Args& a, const SimtPlan&
 
 // Pieces: the number whose blocks fill the SMs best in whole rounds of what is at work at the same time (five blocks of 8 rows to an SM; of
 // 64 rows two with 128 channels, three with 64), a few per cent given away for each more, but none with less than 128 keys where all are
-// there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 953 us; XX.)
+// there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 953 us; by whole rounds 538.)
 SimtPlan simt_plan(int units, int m, int rows, int D) {
     SimtPlan p;
     p.mt = m <= 24 ? 8 : 64;

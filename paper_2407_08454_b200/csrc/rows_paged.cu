@@ -3,7 +3,8 @@
 // the work is a stream of K and V past a handful of queries, bound by bandwidth, and these need neither tensor memory nor a barrier
 // between the two products.
 // Work is dealt to warps: the list of all units' blocks of 16 rows, in equal shares, so that neither lengths that differ nor units that are
-// short leave any idle (a block of four warps per unit and piece of it took 26 us for 512 units of 292 rows, 76 MB; this XX).
+// short leave any idle (a block of four warps per unit and piece of it took 26.5 us for 512 units of 292 rows, 76 MB; this 20.5, of which the
+// stream is 12).
 // A warp copies its own blocks into a ring of its own (TMA, 128-byte swizzle, so that ldmatrix meets no bank conflict), STAGES ahead
 // across the ends of units, and waits for nobody else: 192 KB are in flight per SM.  (Straight from memory into the operands'
 // registers, 8 KB in flight for each of twelve warps: as fast on all SMs, but half the rate per SM, which counts beside a prefix.)

@@ -8,6 +8,8 @@
 //   - The work is a list of items (unit, pair of tiles), each with as many steps as the unit has key tiles, and a CTA takes an
 //     equal share of all steps: a decode batch over one prefix has 8 items for 148 CTAs, a chunk of a prompt 512, lengths differ by unit.
 //     An item that falls into several shares leaves the states of its pieces (O, reference, sums), which another kernel joins.
+//   - Where a unit has one tile of queries only (a few drafted tokens, a small batch over a prefix) both groups work on it, on alternate key
+//     tiles, so that one's exponentials run under the other's products here too; their states are joined like those of pieces.
 //   - The last key tile is cut where the unit ends: logits beyond are -inf, and what V holds there, which may be anything, is kept out
 //     of the product (16 keys at a time; the last ones' rows of V are zeroed in shared memory).
 // Bound by the exponentials and the softmax around them where there are many rows (see prefill_tc.cu for the clocks), by bandwidth where
@@ -48,7 +50,7 @@ struct Args {
     Output out;
     States st;
     const int32_t* len;
-    int rows, units, tiles, whole, direct;      // direct: an item in one piece goes to the output, else to slot 2 * gridDim.x + its number
+    int rows, units, tiles, alt, whole, direct;      // direct: an item in one piece goes to the output, else to slot 2 * gridDim.x + its number
     int R, gx, bx, per_block;           // query rows of a block, a tile's box, tiles per block of more than 128 rows
     int m;                              // query rows of a unit
     float scale2;
@@ -268,16 +270,16 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const uint32_t q_lo = (uint32_t)dq, k_lo = (uint32_t)dk, hi = (uint32_t)(dk >> 32), v_lo = (uint32_t)dv, v_hi = (uint32_t)(dv >> 32);
         uint32_t kv = 0, p_ph = 0, q_ph = 0;                 // iterations before this piece; phases of P and Q (bit g)
         bool ok = true;
-        auto logits = [&](int g, uint32_t x, bool last) {    // S_g = Q_g K^T with K tile number x; the piece's last one
+        auto logits = [&](int g, int qt, uint32_t x, bool last) {         // S_g = Q K^T of Q tile qt with K tile number x; that Q tile's last one
             if (elect_one()) {
 #pragma unroll
                 for (int kc = 0; kc < KCH; ++kc)
 #pragma unroll
                     for (int ks = 0; ks < KCHUNK / 16; ++ks)
-                        umma_bf16_lo(tmem_base + g * S_COLS, q_lo + ((g * TILE_BYTES + kc * CHUNK_BYTES + ks * 32) >> 4), hi,
+                        umma_bf16_lo(tmem_base + g * S_COLS, q_lo + ((qt * TILE_BYTES + kc * CHUNK_BYTES + ks * 32) >> 4), hi,
                                      k_lo + (x % NST) * (TILE_BYTES >> 4) + ((kc * CHUNK_BYTES + ks * 32) >> 4), hi, IDESC_S, (kc | ks) ? 1u : 0u);
                 umma_commit(&sh.bar.s_full[g]);
-                if (last) umma_commit(&sh.bar.q_empty[g]);
+                if (last) umma_commit(&sh.bar.q_empty[qt]);
             }
         };
         // A piece's first logits of a tile come right after the tile's last P V of the piece before (the walk starts with a piece of
@@ -313,8 +315,11 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         __syncwarp();
                     }
                 }
+                // (a single tile: both groups work on it, on alternate key tiles; the next logits are made beside this step's softmax)
+                const int g0 = a.alt ? j & 1 : 0, g1 = a.alt ? g0 + 1 : 1 + both;
+                if (a.alt && ok && j + 1 < len) logits((j + 1) & 1, 0, x + 1, j + 2 == len);
 #pragma unroll 1
-                for (int g = 0; g < 1 + both; ++g) {
+                for (int g = g0; g < g1; ++g) {
                     if (!ok) break;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {            // the first keys' products run while the last ones' P is made
@@ -326,21 +331,23 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                             for (int kk = h ? P_FIRST / 16 : 0; kk < (h ? TILE / 16 : P_FIRST / 16); ++kk)   // 16 keys per MMA: 8 columns of P, 2 KB of V
                                 if (kk < slices)
                                     umma_bf16_ts(tmem_base + O_COL0 + g * D, tmem_base + g * S_COLS + kk * 8,
-                                                 v_lo + s * (TILE_BYTES >> 4) + ((kk * 16 * 128) >> 4), v_hi, IDESC_O, (j | kk) ? 1u : 0u);
-                            if (h && j == len - 1) umma_commit(&sh.bar.o_full[g]);
+                                                 v_lo + s * (TILE_BYTES >> 4) + ((kk * 16 * 128) >> 4), v_hi, IDESC_O, (j > a.alt || kk) ? 1u : 0u);
+                            if (h && j >= len - 1 - a.alt) umma_commit(&sh.bar.o_full[g]);
                         }
                     }
                     if (!ok) break;
                     p_ph ^= 1u << g;
                     const bool more = j + 1 < len;
-                    if (more || (has_next && next_piece_here(g, i))) logits(g, more ? x + 1 : kv + (uint32_t)len, more ? j + 2 == len : nx.steps() == 1);
+                    const int t = a.alt ? 0 : g;             // (of a single tile the other logits have been issued above)
+                    if (more ? !a.alt : has_next && next_piece_here(t, i))
+                        logits(t, t, more ? x + 1 : kv + (uint32_t)len, more ? j + 2 == len : nx.steps() == 1);
                 }
                 if (ok && elect_one()) umma_commit(&sh.bar.kv_empty[s]);
             }
             if (!ok || !has_next) break;
 #pragma unroll 1
             for (int g = len > 0 ? 1 + both : 0; g < 2; ++g)
-                if (next_piece_here(g, i)) logits(g, kv + (uint32_t)len, nx.steps() == 1);
+                if (next_piece_here(g, i)) logits(g, g, kv + (uint32_t)len, nx.steps() == 1);
             if (!ok) break;
             if (elect_one()) umma_commit(&sh.bar.k0_done);
             kv += (uint32_t)len;
@@ -395,12 +402,12 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 }
                 ahead = mine.next(sh.piece[warp]);
             }
-            const int tile = 2 * p.pair + g;
+            const int tile = a.alt ? 0 : 2 * p.pair + g;
             if (tile >= a.tiles) continue;
-            const int k0 = p.k0, k1 = p.k1, last_live = p.k1 == p.nk ? p.n - (p.nk - 1) * TILE : TILE;   // keys of the last step
+            const int k0 = a.alt ? p.k0 + g : p.k0, k1 = p.k1, kstep = 1 + a.alt, last_live = p.k1 == p.nk ? p.n - (p.nk - 1) * TILE : TILE;   // keys of the last step
             float m = LOWEST, l = 0.f, lr = 0.f;             // reference (log2 units); sums relative to it: exact, of the rounded weights
 #pragma unroll 1
-            for (int j = k0; j < k1; ++j) {
+            for (int j = k0; j < k1; j += kstep) {
                 ok = ok && mbar_wait(&sh.bar.s_full[g], s_ph, abort_flag);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
@@ -530,7 +537,8 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 lr = lr * alpha + ((rsum[0] + rsum[1]) + (rsum[2] + rsum[3]));
             }
             // ---- the piece's end
-            ok = ok && mbar_wait(&sh.bar.o_full[g], o_ph, abort_flag);
+            const bool none = k0 >= k1;                      // (a single step is the first group's)
+            ok = ok && (none || mbar_wait(&sh.bar.o_full[g], o_ph, abort_flag));
             ok = __all_sync(0xffffffffu, ok);
             const bool direct = a.direct && p.whole();
             const long long slot = p.whole() ? 2ll * gridDim.x + item : Walk::slot(p);
@@ -549,6 +557,10 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 } else if (!direct) {
                     a.st.ml[srow] = make_float4(0.f, NAN, NAN, 0.f);
                 }
+                continue;
+            }
+            if (none) {
+                a.st.ml[srow] = make_float4(LOWEST, 0.f, 0.f, 0.f);
                 continue;
             }
             o_ph ^= 1;
@@ -674,16 +686,22 @@ TcPlan tc_plan(int units, int R, int N, int rows, bool direct) {
     p.bx = N == 1 ? 1 : TILE / p.gx;
     p.per_block = R > TILE ? (R + TILE - 1) / TILE : 0;
     p.tiles = p.per_block ? N * p.per_block : (N + p.bx - 1) / p.bx;
-    p.direct = direct;
     p.items = (p.tiles + 1) / 2;
     const long long tiles = (rows + TILE - 1) / TILE, all = (long long)units * p.items, steps = all * tiles;
     p.grid = steps < SMS ? (int)steps : SMS;
     // Items stay whole where the fullest CTA then has at most WHOLE steps more than an equal share: what the states of cut items and their
     // joining cost.
     p.whole = (all + p.grid - 1) / p.grid * tiles * p.grid <= steps + WHOLE * p.grid;
+    // (148 units x 256 rows, us without / with, by steps: 1 10.2 / 10.0, 4 16.4 / 17.2, 8 25.2 / 27.2, 24 60.8 / 64.7, the instructions being at hand
+    // from the last launch; between other kernels, 6 steps, 66.6 / 64.1 and 3 steps 37.1 / 35.2.)
     p.compact = steps <= 12 * p.grid;
-    p.slot_rows = p.tiles > 1 ? 2 * TILE : TILE;
-    p.slots = 2ll * p.grid + (direct ? 0 : (long long)units * p.items);
+    // A single tile per unit: both softmax groups on it, each with a state of its own (which are joined, so nothing goes straight to the output).
+    // (us with / without, steps per CTA: 64 units x 20 rows x 14336 keys 48 steps 86.7 / 93.2; 64 x 128 x 3584 12 steps 38.6 / 41.1; 32 x 32 x 3584
+    // 6.3 steps 25.8 / 27.3; 2 x 64 x 28672 3 steps 24.4 / 21.4; beside own rows, 8 x 32 x 14336 6 steps 35.4 / 34.4.  all: what the states take.)
+    p.alt = p.tiles == 1 && !p.whole && all <= 4 * SMS && steps >= (direct ? 6 : 8) * p.grid;
+    p.direct = direct && !p.alt;
+    p.slot_rows = p.tiles > 1 || p.alt ? 2 * TILE : TILE;
+    p.slots = 2ll * p.grid + (p.direct ? 0 : all);
     return p;
 }
 
@@ -696,7 +714,7 @@ cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const 
     mo = mq;                                    // (not used where nothing goes to the output)
     if (plan.direct && !make_map(&mo, out.O, units, q.R, s.D, 32)) return cudaErrorNotSupported;
     Args a;
-    a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.whole = plan.whole; a.direct = plan.direct;
+    a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.whole = plan.whole; a.alt = plan.alt; a.direct = plan.direct;
     a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats; a.own = own;
     auto fn = s.D == 128 ? (plan.compact ? launch_t<2, true> : launch_t<2, false>) : (plan.compact ? launch_t<1, true> : launch_t<1, false>);
     return fn(plan, mq, mk, mv, mo, ms, a, st);

@@ -63,7 +63,7 @@ struct States {
     int stride;
     // Which rows an item holds.  Tiles of `tile` consecutive rows of a unit; or (R > 0) each block of R rows in tiles of its own.
     int tile, R, two;                           // two: two tiles to an item, `tile_room` rows apart
-    int tile_room;
+    int tile_room, halves;                      // halves: a piece has two states, tile_room rows apart
     __device__ __forceinline__ void find(int m, int& item, int& row) const {
         int t, in;
         if (R > 0) {
@@ -182,7 +182,7 @@ struct TcPlan {
     int gx, bx;                                 // rows of a query tile: bx blocks of gx rows
     int per_block, tiles, items;                // tiles of a block of more than 128 rows (else 0), tiles and items (pairs of tiles) of a unit
     int direct, grid, slot_rows;                // direct: an item in one piece goes to the output
-    int compact, whole;                         // few steps per CTA; items are not cut
+    int compact, whole, alt;                    // few steps per CTA; items are not cut; both groups on a single tile: two states per piece
     long long slots;
 };
 TcPlan tc_plan(int units, int R, int N, int rows, bool direct);

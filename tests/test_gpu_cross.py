@@ -78,6 +78,9 @@ SHAPES = [
     (1, 16, 16, 260, 390, 128),
     (3, 8, 8, 300, 1000, 128),            # more steps than SMs: shares that hold whole items and parts
     (6, 8, 4, 200, 700, 64),
+    (1, 2, 1, 7, 4000, 128),              # one tile, keys in many pieces of one step
+    (12, 8, 8, 9, 2600, 128),             # ... of several steps
+    (30, 4, 4, 100, 2000, 64),
 ]
 
 

@@ -85,7 +85,21 @@ SHAPES = [
 ]
 
 
-@pytest.mark.parametrize("B,Hq,Hkv,D,prefix,held,R", SHAPES)
+# Batches for which the prefix has a kernel of its own (reading it again for every sequence would cost more): tiles of query rows that hold
+# whole blocks of heads or a part of one, one tile, a pair, several; with and without own rows beside it.
+LARGE = [
+    (64, 40, 2, 128, 200, 33, 16),
+    (16, 136, 1, 128, 400, 20, 16),
+    (70, 32, 4, 128, 300, 17, 32),
+    (100, 12, 3, 64, 600, 40, 16),
+    (130, 6, 2, 128, 300, 0, 16),
+    (40, 4, 4, 128, 1700, 30, 16),         # one tile of 40 rows, pieces of several steps
+    (33, 8, 8, 64, 2100, 5, 64),
+    (128, 1, 1, 128, 530, 12, 16),         # exactly one tile
+]
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,prefix,held,R", SHAPES + LARGE)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_shared_matches_64_bits(B, Hq, Hkv, D, prefix, held, R, dtype):
     check(B, Hq, Hkv, D, prefix, held, R, dtype)

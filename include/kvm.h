@@ -375,8 +375,8 @@ int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, 
  *   K_pre, V_pre NULL (no prefix: decode attention over a paged cache), or [n_kv_heads, pre_rows, D] in p->dtype, as
  *                kvm_compress leaves them for a batch of one; pre_rows <= KVM_MAX_ROWS
  *   pre_len      NULL (every KV head holds pre_rows rows) or device [n_kv_heads] i32 (clamped to 0..pre_rows)
- *   own          NULL (no rows beside the prefix), or the paged cache of the sequences' own rows; not written.  batch * n_q_heads times
- *                max_pages * page_rows / 16 must stay below 2^31 (KVM_E_SHAPE)
+ *   own          NULL (no rows beside the prefix), or the paged cache of the sequences' own rows; not written.  batch * n_q_heads *
+ *                (max_pages * page_rows + pre_rows) / 16 must stay below 2^31 (KVM_E_SHAPE)
  *   out          [batch, n_q_heads, D] in p->dtype, written: softmax over the prefix's and the own rows together; zeros where there
  *                are none; NaN where a bounded wait inside the kernel gave up
  * bf16: fp32 accumulation and softmax, the weights enter the product with V rounded to bf16 and are divided by the sum of the

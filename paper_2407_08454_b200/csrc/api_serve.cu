@@ -43,7 +43,9 @@ int derive(const kvm_pages* c, bool sizes_only, Pages& o) {
 }
 
 // (Blocks of 16 rows are counted in 32 bits.)
-bool too_many(const Shape& s, const Pages& c) { return (long long)s.B * s.Hq * (c.room() / 16) >= (1ll << 31); }
+bool too_many(const Shape& s, int pre_rows, const Pages* c) {
+    return (long long)s.B * s.Hq * ((c ? c->room() / 16 : 0) + (pre_rows + 15) / 16) >= (1ll << 31);
+}
 
 struct Carver {
     char* base;
@@ -233,7 +235,7 @@ int kvm_shared_workspace_bytes(const kvm_params* p, int32_t pre_rows, const kvm_
     if (!bytes) return KVM_E_NULL;
     if (pre_rows < 0 || pre_rows > KVM_MAX_ROWS || (pre_rows == 0 && !own)) return KVM_E_SHAPE;
     if (own && (rc = derive(own, true, pg)) != KVM_OK) return rc;
-    if (own && too_many(s, pg)) return KVM_E_SHAPE;
+    if (too_many(s, pre_rows, own ? &pg : nullptr)) return KVM_E_SHAPE;
     *bytes = plan_shared(s, pre_rows, own ? &pg : nullptr, nullptr).bytes;
     return KVM_OK;
 }
@@ -248,7 +250,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (!q || !out || !K_pre != !V_pre || (!K_pre && !own)) return KVM_E_NULL;
     if (K_pre ? (pre_rows < 1 || pre_rows > KVM_MAX_ROWS) : pre_rows != 0) return KVM_E_SHAPE;
     if (own && (rc = derive(own, false, pg)) != KVM_OK) return rc;
-    if (own && too_many(s, pg)) return KVM_E_SHAPE;
+    if (too_many(s, pre_rows, own ? &pg : nullptr)) return KVM_E_SHAPE;
     if (misaligned(q) || misaligned(out) || (K_pre && (misaligned(K_pre) || misaligned(V_pre))) || (pre_len && misaligned(pre_len, 4)))
         return KVM_E_ALIGN;
     const SharedWork w = plan_shared(s, pre_rows, own ? &pg : nullptr, ws);
@@ -258,7 +260,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     const Output o = {out, nullptr, nullptr, nullptr};
     const Queries pre_q = {q, s.G, s.Hq, s.G, s.B}, own_q = {q, s.G, 0, s.G, 1};
     const Keys pre_k = {K_pre, V_pre, pre_len, pre_rows, nullptr, 0, 0, 0};
-    const Keys own_k = {pg.K, pg.V, pg.len, own ? pg.room() : 0, pg.table, pg.n_pages, pg.shift, pg.max_pages};
+    const Keys own_k = {pg.K, pg.V, pg.len, own ? pg.room() : 0, pg.table, pg.n_pages, own ? pg.shift : 4, pg.max_pages};
     if (w.fold) {
         const Fold f = {K_pre, V_pre, pre_len, s.Hkv, pre_rows};
         if (launch_rows_paged(s, w.own_paged, q, own_k, f, Beside{}, w.own_states, out, stats, st) != cudaSuccess) return KVM_E_CUDA;

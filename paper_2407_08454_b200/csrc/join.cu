@@ -196,19 +196,19 @@ join_items_kernel(const States a, const int32_t* __restrict__ len, const Output 
     const int4 pc = __ldcg(a.pieces + at);
     if (n > 0 && pc.x == 1 && !a.halves) return;
     Pieces p = {n > 0 ? pc.x << (a.halves ? 1 : 0) : 0, pc.y, pc.z, a.stride, a.o, a.ml, a.rows, a.halves ? a.tile_room : 0}, none = {};
-    if (ITEM_ROWS == 1) {
+    if constexpr (ITEM_ROWS == 1) {
         p.o = a.o + (size_t)part * D;
         p.ml = a.ml + part;
         Sum<D / 32> s = sum_pieces<D>(p, none, threadIdx.x >> 5, JOIN_NT / 32);
         join_warps<D>(s);
         if (threadIdx.x < 32) store_row<T, D>(s, out, (long long)u * m_rows + m0);
-        return;
-    }
+    } else {
 #pragma unroll 1
-    for (int r = threadIdx.x >> 5; r < ITEM_ROWS && m0 + r < m_rows; r += JOIN_NT / 32) {
-        p.o = a.o + (size_t)(part * ITEM_ROWS + r) * D;
-        p.ml = a.ml + part * ITEM_ROWS + r;
-        store_row<T, D>(sum_pieces<D>(p, none, 0, 1), out, (long long)u * m_rows + m0 + r);
+        for (int r = threadIdx.x >> 5; r < ITEM_ROWS && m0 + r < m_rows; r += JOIN_NT / 32) {
+            p.o = a.o + (size_t)(part * ITEM_ROWS + r) * D;
+            p.ml = a.ml + part * ITEM_ROWS + r;
+            store_row<T, D>(sum_pieces<D>(p, none, 0, 1), out, (long long)u * m_rows + m0 + r);
+        }
     }
 }
 

@@ -3,12 +3,13 @@
 // with one pass over the keys, a running maximum and sum per row, and, where there are few rows, the keys cut into pieces whose
 // states are joined by another kernel.
 //
-// Two forms.  Up to 24 query rows per unit (a decode step): blocks of 8 rows, 32 keys at a time, bound by bandwidth: a pair of
+// Two forms.  Up to 16 query rows per unit (a decode step): blocks of 8 rows, 32 keys at a time, bound by bandwidth: a pair of
 // rows reads a key's channels from shared memory once, 64 KB of shared-memory reads for 32 KB of keys and values and each
-// product (about 1,100 clocks against 1,400 that an SM's share of the bandwidth takes).  More rows: blocks of 64 rows by 64 keys
-// (32 with 128 channels), four rows per thread, bound by the fp32 pipes and shared memory together.
-// (8 heads over 4096 keys, D = 64 / 128, us: 32 rows by eights 38.4 / 54, 48 rows 46.5 / 76, 64 rows together 33.6 / 48.5.)
+// product (about 1,100 clocks against 1,400 that an SM's share of the bandwidth takes).  More rows: blocks of 64 rows by 32 keys
+// on warp-level matrix products of three bf16 planes, bound by those.
 // The next keys are on their way to registers while the current ones are used.
+#include <mutex>
+
 #include "serve.cuh"
 #include "tc_common.cuh"
 
@@ -16,7 +17,7 @@ namespace kvm {
 namespace serve {
 namespace {
 
-constexpr int NT8 = 256, NT64 = 256;        // threads of a block of 8 and of 64 query rows
+constexpr int NT8 = 256, NT64 = 128;        // threads of a block of 8 and of 64 query rows
 
 struct Args {
     Queries q;
@@ -194,138 +195,211 @@ template <typename T, int D> __global__ void __launch_bounds__(NT8) rows8_kernel
 }
 
 // ------------------------------------------------------------------ many rows
-// A thread takes four rows by KT / 16 keys, then four rows by D / 16 channels, pairs of channels in one instruction.  28.7 TFLOP/s of 72 with
-// 64 channels, 30.1 with 128 (16 heads x 1024 queries x 2048 keys); eight rows per thread of half as many, which halves the
-// reads per product, is as fast (27.9, 30.0), and so are single products: neither the reads nor the issue slots bound it.
-template <int D> constexpr int keys64() { return D == 128 ? 32 : 64; }
-template <int D> constexpr size_t rows64_smem() { return ((64 + 2 * keys64<D>()) * (D + 4) + 64 * (keys64<D>() + 4)) * sizeof(float); }
-template <typename T, int D> __global__ void __launch_bounds__(NT64) rows64_kernel(const Args a) {
-    constexpr int MT = 64, KT = keys64<D>(), P = D + 4, PP = KT + 4, E = D / 16, KJ = KT / 16, R = 4;
-    extern __shared__ __align__(16) float smem[];
-    float *sq = smem, *sk = sq + MT * P, *sv = sk + KT * P, *sp = sv + KT * P;
-    const int rg = threadIdx.x / 16, kg = threadIdx.x % 16;              // four rows; keys kg + 16 j, channels 4 kg + 64 j
-    const int u = blockIdx.z, m0 = blockIdx.x * MT;
+// On warp-level matrix products: an fp32 number is the sum of three bf16 numbers (each rounded to the nearest, what is left after two is below
+// 2^-17 of it and after three below 2^-26), and of the nine products of two such sums the six that reach 2^-26 are kept:
+//   x y = x1 y1 + (x1 y2 + x2 y1) + (x1 y3 + x2 y2 + x3 y1),
+// accumulated in fp32, the small ones first.  A warp has 16 query rows, whose three planes stay in registers; the block's four warps share
+// the planes of 32 keys and values, made while they are written to shared memory (16-byte pieces swizzled by the row, so that ldmatrix
+// meets no bank conflict).  The weights are split in registers: what a lane holds of the first product is what it needs for the second.
+// (By products on the fp32 pipes, 64 x 64 blocks: 28.7 TFLOP/s with 64 channels, 31.9 with 128; this 43.6 and 43.0, which is
+// 260 of bf16 products: 16 heads x 1024 queries x 2048 keys.)
+constexpr int KEYS = 32;
+// Three planes of two numbers, packed in pairs.  (An infinite number's rest would be NaN: it is none.)
+__device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        p[i] = Vec<__nv_bfloat16>::pack2(x, y);
+        if (i == 2) break;
+        const float a = __uint_as_float(p[i] << 16), b = __uint_as_float(p[i] & 0xffff0000u);
+        x = fabsf(a) == INFINITY ? 0.f : x - a;
+        y = fabsf(b) == INFINITY ? 0.f : y - b;
+    }
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows64_kernel(const Args a) {
+    constexpr int MT = 64, KS = D / 16, PLANE = KEYS * D * 2;            // a plane of the keys or values, bytes
+    constexpr bool AHEAD = D == 64;                                      // (with 128 channels the next keys would not fit beside the rest)
+    extern __shared__ __align__(128) uint8_t smem[];                     // [K | V][plane][key][D]
+    __shared__ bool slive[KEYS];
+    const uint32_t base = tc::smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    const int u = blockIdx.z, m0 = blockIdx.x * MT + warp * 16;          // this warp's first row
     grid_dependency_wait();
     int r0, r1;
-    share<KT>(a, u, r0, r1);
-    load_queries<T, D, MT, NT64>(a, u, m0, sq, P);
-    Tile<T, D, KT, NT64> t;
-    t.load(a.k, u, r0, r1);
-    float m[R], l[R] = {};                                               // l: of this thread's keys
-    uint64_t o[R][E / 2] = {};                                           // pairs of channels
+    share<KEYS>(a, u, r0, r1);
+    Tile<float, D, KEYS, NT64> t;
+    if (AHEAD) t.load(a.k, u, r0, r1);
+    uint32_t q[KS][3][4];                                                // planes of rows gid, gid + 8: the first operand
 #pragma unroll
-    for (int i = 0; i < R; ++i) m[i] = -INFINITY;
-    for (int r = r0; r < r1; r += KT) {
+    for (int h = 0; h < 2; ++h) {
+        const int m = m0 + gid + h * 8;
+        const float* row = (const float*)a.q.q + a.q.at(u, min(m, a.q.rows() - 1)) * D + 2 * tig;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float2 f = __ldg(reinterpret_cast<const float2*>(row + ks * 16 + x * 8));
+                uint32_t pl[3];
+                split2(f.x * a.scale2, f.y * a.scale2, pl);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) q[ks][i][x * 2 + h] = pl[i];
+            }
+    }
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[D / 8][4]; // rows gid, gid + 8 (l: of this lane's keys); channels 8 j + 2 tig, + 1
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    // (the planes that a product takes: small ones first)
+    constexpr int PA[6] = {2, 1, 0, 1, 0, 0}, PB[6] = {0, 1, 2, 0, 1, 0};
+    for (int r = r0; r < r1; r += KEYS) {
         __syncthreads();
-        t.store(sk, sv);
-        __syncthreads();
-        if (r + KT < r1) t.load(a.k, u, r + KT, r1);
-        uint64_t x2[R][KJ] = {};
-#pragma unroll 2
-        for (int c = 0; c < D; c += 4) {
-            ulonglong2 kv[KJ];
+        if (!AHEAD) t.load(a.k, u, r, r1);
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) kv[j] = *reinterpret_cast<const ulonglong2*>(sk + (kg + 16 * j) * P + c);
+        for (int i = 0; i < t.PER; ++i) {
+            const int key = (threadIdx.x + i * NT64) / t.LPR, c = (threadIdx.x + i * NT64) % t.LPR * 4;
+            uint8_t* at = smem + key * (D * 2) + ((((c >> 3) ^ (key & 7)) << 4) | ((c & 4) << 1));
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const ulonglong2 qv = *reinterpret_cast<const ulonglong2*>(sq + (rg * R + i) * P + c);
+            for (int kv = 0; kv < 2; ++kv) {
+                const uint4 f = kv ? t.v[i] : t.k[i];
+                uint32_t lo[3], hi[3];
+                split2(__uint_as_float(f.x), __uint_as_float(f.y), lo);
+                split2(__uint_as_float(f.z), __uint_as_float(f.w), hi);
 #pragma unroll
-                for (int j = 0; j < KJ; ++j) x2[i][j] = tc::ffma2(qv.y, kv[j].y, tc::ffma2(qv.x, kv[j].x, x2[i][j]));
+                for (int pl = 0; pl < 3; ++pl) *reinterpret_cast<uint2*>(at + (kv * 3 + pl) * PLANE) = make_uint2(lo[pl], hi[pl]);
             }
         }
-        float x[R][KJ];
+        if (threadIdx.x < KEYS) slive[threadIdx.x] = r + (int)threadIdx.x < r1 && exists(a, u, r + threadIdx.x);
+        __syncthreads();
+        if (AHEAD && r + KEYS < r1) t.load(a.k, u, r + KEYS, r1);
+        // ---- logits: 16 rows x 32 keys
+        float x[4][4];                                                   // keys 8 n + 2 tig, + 1 of rows gid (first two), gid + 8
 #pragma unroll
-        for (int i = 0; i < R; ++i)
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) {
-                float lo, hi;
-                tc::unpack2(x2[i][j], lo, hi);
-                x[i][j] = lo + hi;
-            }
-        bool live[KJ];
+            for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
 #pragma unroll
-        for (int j = 0; j < KJ; ++j) live[j] = r + kg + 16 * j < r1 && exists(a, u, r + kg + 16 * j);
+        for (int ks = 0; ks < KS; ++ks) {
+            uint32_t kf[3][2][4];                                        // plane, 16 keys: channels 0..7, 8..15 of the first 8, of the last 8
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            float mn = -INFINITY;
+            for (int pl = 0; pl < 3; ++pl)
 #pragma unroll
-            for (int j = 0; j < KJ; ++j) {
-                if (!live[j]) x[i][j] = -INFINITY;
-                mn = fmaxf(mn, x[i][j]);
-            }
-#pragma unroll
-            for (int z = 8; z > 0; z >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, z));
-            mn = fmaxf(mn, m[i]);
-            const float alpha = rescale2(m[i], mn);
-            m[i] = mn;
-            l[i] *= alpha;
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) {
-                const float p = rescale2(x[i][j], mn);
-                l[i] += p;
-                sp[(rg * R + i) * PP + kg + 16 * j] = p;
-            }
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) o[i][e] = tc::fmul2(o[i][e], tc::pack2(alpha, alpha));
-        }
-        __syncwarp();                                                    // (a warp reads the weights of its own rows only)
-#pragma unroll 1
-        for (int j = 0; j < KT; j += 4) {
-            ulonglong2 v[4][E / 4];
-#pragma unroll
-            for (int jj = 0; jj < 4; ++jj)
-#pragma unroll
-                for (int x4 = 0; x4 < E / 4; ++x4) v[jj][x4] = *reinterpret_cast<const ulonglong2*>(sv + (j + jj) * P + kg * 4 + x4 * 64);
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const float4 p4 = *reinterpret_cast<const float4*>(sp + (rg * R + i) * PP + j);
-#pragma unroll
-                for (int jj = 0; jj < 4; ++jj) {
-                    const float p = jj == 0 ? p4.x : jj == 1 ? p4.y : jj == 2 ? p4.z : p4.w;
-                    const uint64_t p2 = tc::pack2(p, p);
-#pragma unroll
-                    for (int x4 = 0; x4 < E / 4; ++x4) {
-                        o[i][x4 * 2] = tc::ffma2(p2, v[jj][x4].x, o[i][x4 * 2]);
-                        o[i][x4 * 2 + 1] = tc::ffma2(p2, v[jj][x4].y, o[i][x4 * 2 + 1]);
-                    }
+                for (int h = 0; h < 2; ++h) {
+                    const int key = h * 16 + (lane & 7) + ((lane >> 4) << 3), piece = ks * 2 + ((lane >> 3) & 1);
+                    ldsm4(kf[pl][h], base + pl * PLANE + key * (D * 2) + ((piece ^ (key & 7)) << 4));
                 }
+#pragma unroll
+            for (int i = 0; i < 6; ++i)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) mma16816(x[n], q[ks][PA[i]], kf[PB[i]][n >> 1][(n & 1) * 2], kf[PB[i]][n >> 1][(n & 1) * 2 + 1]);
+        }
+        // ---- weights
+        float mn[2] = {m[0], m[1]};
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!slive[n * 8 + 2 * tig + (e & 1)]) x[n][e] = -INFINITY;
+                mn[e >> 1] = fmaxf(mn[e >> 1], x[n][e]);
+            }
+        float alpha[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            mn[h] = fmaxf(mn[h], __shfl_xor_sync(0xffffffffu, mn[h], 1));
+            mn[h] = fmaxf(mn[h], __shfl_xor_sync(0xffffffffu, mn[h], 2));
+            alpha[h] = rescale2(m[h], mn[h]);
+            m[h] = mn[h];
+            l[h] *= alpha[h];
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[n][e] = rescale2(x[n][e], m[e >> 1]);
+                l[e >> 1] += x[n][e];
+            }
+        if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f))
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][e] *= alpha[e >> 1];
+        // ---- the weighted sum, 16 keys at a time
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            uint32_t w[3][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t pl[3];
+                split2(x[2 * kt + (e >> 1)][(e & 1) * 2], x[2 * kt + (e >> 1)][(e & 1) * 2 + 1], pl);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) w[i][e] = pl[i];
+            }
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) {
+                uint32_t vf[3][4];                                       // plane: 16 keys of channels 16 j .. + 8, and of the next 8
+#pragma unroll
+                for (int pl = 0; pl < 3; ++pl) {
+                    const int key = kt * 16 + (lane & 15), piece = j * 2 + (lane >> 4);
+                    ldsm4_t(vf[pl], base + (3 + pl) * PLANE + key * (D * 2) + ((piece ^ (key & 7)) << 4));
+                }
+#pragma unroll
+                for (int i = 0; i < 6; ++i)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) mma16816(o[2 * j + z], w[PA[i]], vf[PB[i]][z * 2], vf[PB[i]][z * 2 + 1]);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
+    for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        const int row = warp * 16 + gid + h * 8, mr = blockIdx.x * MT + row;
+        if (mr >= a.q.rows()) continue;
 #pragma unroll
-        for (int z = 8; z > 0; z >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], z);
-        const int row = rg * R + i;
-        if (m0 + row >= a.q.rows()) continue;
-#pragma unroll
-        for (int x4 = 0; x4 < E / 4; ++x4) {
-            float f[4];
-            tc::unpack2(o[i][x4 * 2], f[0], f[1]);
-            tc::unpack2(o[i][x4 * 2 + 1], f[2], f[3]);
-            finish<T, D, 4>(a, u, blockIdx.x, blockIdx.y, row, m0 + row, kg * 4 + x4 * 64, f, m[i], l[i]);
-        }
+        for (int j = 0; j < D / 8; ++j) finish<float, D, 2>(a, u, blockIdx.x, blockIdx.y, row, mr, j * 8 + 2 * tig, &o[j][2 * h], m[h], l[h]);
     }
 }
 
-template <typename T, int D> cudaError_t launch_t(const Args& a, const SimtPlan& plan, int units, cudaStream_t st) {
+template <int D> cudaError_t launch_t(const Args& a, const SimtPlan& plan, int units, cudaStream_t st) {
     const dim3 grid(plan.items, plan.pieces, units);
-    if (plan.mt == 8) return launch_dependent(rows8_kernel<T, D>, grid, dim3(NT8), 0, st, a);
-    constexpr size_t smem = rows64_smem<D>();
-    // (asked for on every call: the attribute is the current device's, and setting it costs less than keeping track of devices)
-    const cudaError_t e = cudaFuncSetAttribute(rows64_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (plan.mt == 8) return launch_dependent(rows8_kernel<float, D>, grid, dim3(NT8), 0, st, a);
+    constexpr size_t smem = 6 * KEYS * D * 2;                            // (48 KB of planes and what is static: an opt-in)
+    static std::mutex mu;
+    static bool ready[KVM_MAX_DEVICES] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    return launch_dependent(rows64_kernel<T, D>, grid, dim3(NT64), smem, st, a);
+    if (dev < 0 || dev >= KVM_MAX_DEVICES) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready[dev]) {
+            if ((e = cudaFuncSetAttribute(rows64_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+            ready[dev] = true;
+        }
+    }
+    return launch_dependent(rows64_kernel<D>, grid, dim3(NT64), smem, st, a);
 }
 
 }  // namespace
 
 // Pieces: the number whose blocks fill the SMs best in whole rounds of what is at work at the same time (five blocks of 8 rows to an SM; of
 // 64 rows two with 128 channels, three with 64), a few per cent given away for each more, but none with less than 128 keys where all are
-// there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 953 us; by whole rounds 538.)
+// there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 1.8 times what whole rounds take.)
 SimtPlan simt_plan(int units, int m, int rows, int D) {
     SimtPlan p;
-    p.mt = m <= 24 ? 8 : 64;
+    p.mt = m <= 16 ? 8 : 64;
     p.items = (m + p.mt - 1) / p.mt;
     const long long blocks = (long long)units * p.items, room = SMS * (p.mt == 8 ? 5 : D == 128 ? 2 : 3);
     const long long most = ((long long)rows + 127) / 128, least = (room + blocks - 1) / blocks;     // (least: one round, more or less)
@@ -342,7 +416,7 @@ cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, co
                              kvm_stats* stats, cudaStream_t st) {
     if (units > 65535 || plan.pieces > 65535) return cudaErrorInvalidValue;
     const Args a = {q, k, states, out, stats, s.scale * LOG2E, plan.pieces};
-    return s.D == 128 ? launch_t<float, 128>(a, plan, units, st) : launch_t<float, 64>(a, plan, units, st);
+    return s.D == 128 ? launch_t<128>(a, plan, units, st) : launch_t<64>(a, plan, units, st);
 }
 
 }  // namespace serve

@@ -51,7 +51,7 @@ struct Args {
     States st;
     const int32_t* len;
     int rows, units, tiles, alt, whole, direct;      // direct: an item in one piece goes to the output, else to slot 2 * gridDim.x + its number
-    int R, gx, bx, per_block;           // query rows of a block, a tile's box, tiles per block of more than 128 rows
+    int gx, bx, per_block;              // a tile's box, tiles per block of more than 128 rows
     int m;                              // query rows of a unit
     float scale2;
     kvm_stats* stats;
@@ -358,19 +358,20 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         // ============================== units without keys ==============================
         // (where items are cut, the kernel that joins their pieces sees to these)
         if (a.whole && a.direct && a.len)
-            for (int u = blockIdx.x; u < a.units; u += gridDim.x) {
-                if (walk.rows_of(u) > 0) continue;
-                for (int r = 0; r < a.m; ++r) {
-                    const long long at = (long long)u * a.m + r;
-                    const float z = a.out.lse_in ? a.out.lse_in[at] : -INFINITY;
-                    if (lane * 8 < D) {
-                        uint4 x = make_uint4(0, 0, 0, 0);
-                        if (z != -INFINITY) x = __ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out.O_in + at * D) + lane);
-                        reinterpret_cast<uint4*>((__nv_bfloat16*)a.out.O + at * D)[lane] = x;
+            for (int u0 = 0; u0 < a.units; u0 += 32) {
+                uint32_t empty = __ballot_sync(0xffffffffu, u0 + lane < a.units && walk.rows_of(min(u0 + lane, a.units - 1)) == 0);
+                for (; empty; empty &= empty - 1)
+                    for (int r = blockIdx.x; r < a.m; r += gridDim.x) {      // every CTA a part of the unit's rows
+                        const long long at = (long long)(u0 + __ffs(empty) - 1) * a.m + r;
+                        const float z = a.out.lse_in ? a.out.lse_in[at] : -INFINITY;
+                        if (lane * 8 < D) {
+                            uint4 x = make_uint4(0, 0, 0, 0);
+                            if (z != -INFINITY) x = __ldcg(reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.out.O_in + at * D) + lane);
+                            reinterpret_cast<uint4*>((__nv_bfloat16*)a.out.O + at * D)[lane] = x;
+                        }
+                        __syncwarp();
+                        if (lane == 0) a.out.lse[at] = z;
                     }
-                    __syncwarp();
-                    if (lane == 0) a.out.lse[at] = z;
-                }
             }
       }
     } else {
@@ -715,7 +716,7 @@ cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const 
     if (plan.direct && !make_map(&mo, out.O, units, q.R, s.D, 32)) return cudaErrorNotSupported;
     Args a;
     a.out = out; a.st = states; a.len = k.len; a.rows = k.rows; a.units = units; a.tiles = plan.tiles; a.whole = plan.whole; a.alt = plan.alt; a.direct = plan.direct;
-    a.R = q.R; a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats; a.own = own;
+    a.gx = plan.gx; a.bx = plan.bx; a.per_block = plan.per_block; a.m = q.rows(); a.scale2 = s.scale * LOG2E; a.stats = stats; a.own = own;
     auto fn = s.D == 128 ? (plan.compact ? launch_t<2, true> : launch_t<2, false>) : (plan.compact ? launch_t<1, true> : launch_t<1, false>);
     return fn(plan, mq, mk, mv, mo, ms, a, st);
 }

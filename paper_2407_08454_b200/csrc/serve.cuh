@@ -86,8 +86,6 @@ struct Output {
     const float* lse_in;
 };
 
-inline size_t state_bytes(size_t slots, int rows, int D) { return slots * rows * ((size_t)D * 4 + sizeof(float4)); }
-
 // Weight of a state with reference m under the reference M (an empty state has m = -inf).
 __device__ __forceinline__ float rescale2(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
 

@@ -211,3 +211,78 @@ def test_calls_on_several_streams_at_once():
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert torch.equal(o, w)
+
+
+def test_prefix_and_own_rows_side_by_side():
+    """A batch large enough for the prefix to have a kernel of its own, which runs beside the one for the sequences' rows: captured and replayed, and
+    from two streams at once, it gives the bits of the plain call, which are right."""
+    g = torch.Generator().manual_seed(31)
+    B, Hq, Hkv, D, P, held, R = 64, 8, 2, 128, 1200, 100, 16
+    p = kvm.make_params(B, Hq, Hkv, 1, D, torch.bfloat16)
+    lengths = torch.randint(0, held + 1, (B, Hkv), generator=g, dtype=torch.int32)
+    K, V, table = make_cache(g, B, Hkv, D, R, lengths, torch.bfloat16)
+    own = kvm.make_pages(K.cuda(), V.cuda(), table.cuda(), lengths.cuda())
+    Kp, Vp = (torch.randn(Hkv, P, D, generator=g).bfloat16() for _ in range(2))
+    n_pre = torch.tensor([P, 900], dtype=torch.int32)
+    q = [torch.randn(B, Hq, D, generator=g).bfloat16() for _ in range(2)]
+    qd, Kd, Vd, nd = [x.cuda() for x in q], Kp.cuda(), Vp.cuda(), n_pre.cuda()
+    n = kvm.kvm_shared_workspace_bytes(p, P, own)
+    ws = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in q]
+    want = []
+    for x, w in zip(qd, ws):
+        out = torch.empty_like(x)
+        kvm.kvm_shared_attend(p, x, Kd, Vd, nd, own, out, w)
+        want.append(out)
+    torch.cuda.synchronize()
+    G = Hq // Hkv
+    for b in range(0, B, 7):
+        for h in range(Hkv):
+            rows = torch.arange(int(lengths[b, h]))
+            page = table[b * Hkv + h][rows // R].long()
+            ref = Rows(q[0][b, h * G:(h + 1) * G], torch.cat([Kp[h, :int(n_pre[h])], K[page, rows % R]]),
+                       torch.cat([Vp[h, :int(n_pre[h])], V[page, rows % R]]), 1.0 / math.sqrt(D))
+            close(want[0][b, h * G:(h + 1) * G], ref.O, ref.O_bound(torch.bfloat16), (b, h))
+    out = torch.empty_like(want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            kvm.kvm_shared_attend(p, qd[0], Kd, Vd, nd, own, out, ws[0])
+    for _ in range(10):
+        out.fill_(math.nan)
+        graph.replay()
+        assert torch.equal(out, want[0])
+    streams, outs = [torch.cuda.Stream() for _ in q], [torch.empty_like(x) for x in qd]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for x, w, o, s in zip(qd, ws, outs, streams):
+            kvm.kvm_shared_attend(p, x, Kd, Vd, nd, own, o, w, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
+def test_rows_behind_the_outputs_are_left_as_they_were():
+    """Outputs that lie inside larger buffers: what surrounds them keeps its bits (tiles and boxes end past the last row)."""
+    g = torch.Generator().manual_seed(32)
+    for dtype in (torch.bfloat16, torch.float32):
+        for B, Hq, Hkv, n, rows, D in ((2, 6, 2, 43, 300, 128), (3, 4, 4, 1, 77, 64), (1, 3, 1, 200, 2600, 64)):
+            p = kvm.make_params(B, Hq, Hkv, 1, D, dtype)
+            Q = torch.randn(B, Hq, n, D, generator=g).to(dtype).cuda()
+            K, V = (torch.randn(B, Hkv, rows, D, generator=g).to(dtype).cuda() for _ in range(2))
+            size, pad = Q.numel(), 64 * D
+            buf, lbuf = torch.full((size + 2 * pad,), 7.0, dtype=dtype, device="cuda"), torch.full((B * Hq * n + 256,), 7.0, device="cuda")
+            O, lse = buf[pad:pad + size].view(Q.shape), lbuf[128:128 + B * Hq * n].view(B, Hq, n)
+            ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n, rows) + 256, dtype=torch.uint8, device="cuda")
+            need = ws.numel() - 256
+            ws[need:] = 99
+            kvm.kvm_cross_attend(p, Q, K, V, None, O, lse, ws[:need])
+            assert (buf[:pad] == 7).all() and (buf[pad + size:] == 7).all()
+            assert (lbuf[:128] == 7).all() and (lbuf[128 + lse.numel():] == 7).all() and (ws[need:] == 99).all()
+            if n == 1:                                  # a decode step, the same
+                q, ob = Q[:, :, 0].contiguous(), torch.full((B * Hq * D + 2 * pad,), 7.0, dtype=dtype, device="cuda")
+                out = ob[pad:pad + B * Hq * D].view(B, Hq, D)
+                Kp, Vp = K[0].contiguous(), V[0].contiguous()
+                ws = torch.empty(kvm.kvm_shared_workspace_bytes(p, rows, None) + 256, dtype=torch.uint8, device="cuda")
+                ws[-256:] = 99
+                kvm.kvm_shared_attend(p, q, Kp, Vp, None, None, out, ws[:-256])
+                assert (ob[:pad] == 7).all() and (ob[pad + out.numel():] == 7).all() and (ws[-256:] == 99).all()

@@ -264,6 +264,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (w.fold) {
         const Fold f = {K_pre, V_pre, pre_len, s.Hkv, pre_rows};
         if (launch_rows_paged(s, w.own_paged, q, own_k, f, Beside{}, w.own_states, out, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.own_paged.alone) return KVM_OK;
         return launch_join(s, s.U, s.G, &w.own_states, nullptr, nullptr, 1, w.own_paged.grid * 4 / w.own_paged.items, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
     if (s.dtype == KVM_BF16) {
@@ -274,7 +275,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
         if (w.pre && launch_rows_simt(s, w.pre_plan, s.Hkv, pre_q, pre_k, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
         if (w.own && launch_rows_simt(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
-    if (!w.pre_states.o && !w.own_states.o) return KVM_OK;
+    if ((!w.pre_states.o && !w.own_states.o) || w.own_paged.alone) return KVM_OK;
     const int about = s.dtype == KVM_BF16 ? (w.own ? w.own_paged.grid * 4 / w.own_paged.items : 0) + (w.pre ? w.pre_tc.grid / (s.Hkv * w.pre_tc.items) : 0)
                                           : w.own_plan.pieces + w.pre_plan.pieces;
     return launch_join(s, s.U, s.G, w.own ? &w.own_states : nullptr, w.pre ? &w.pre_states : nullptr, pre_len, !w.pre, about, o, st) == cudaSuccess

@@ -10,7 +10,8 @@
 // registers, 8 KB in flight for each of twelve warps: as fast on all SMs, but half the rate per SM, which counts beside a prefix.)
 // 16 rows never cross a page (pages are powers of two from 16); page numbers are read a block ahead of the copies.
 // A prefix may be folded in: its rows are then the first of every unit (read once per sequence, through L2).
-// A unit's part of a share leaves its state, which another kernel joins (a unit that is whole may go to the output).
+// A unit's part of a share leaves its state, which another kernel joins (a unit that is whole may go to the output).  Where units are few or
+// short each has a block of its own instead, and no second kernel.
 // Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones.
 #include <mutex>
 
@@ -71,7 +72,8 @@ struct Cursor {
     int left;                               // blocks of the share from this one on; 0: past the end
 };
 
-template <int D> __global__ void __launch_bounds__(NT, PER_SM)
+// ALONE: a block per item, its warps on a quarter of the unit's blocks each, whose states are joined in shared memory: no second kernel.
+template <int D, bool ALONE> __global__ void __launch_bounds__(NT, PER_SM)
 rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_pk,
                   const __grid_constant__ CUtensorMap map_pv, const __grid_constant__ Args a) {
     constexpr int STAGES = stages<D>(), KCH = D / 64;              // 64-channel (128-byte) column chunks
@@ -80,8 +82,10 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full[WARPS][STAGES];
     __shared__ volatile int s_bad;
+    constexpr int LENGTHS = ALONE ? 1 : KEPT;
     __shared__ long long sm_all[WARPS];
-    __shared__ int sm_sum[WARPS], sm_start, sm_item, sm_rows[KEPT], sm_pre[KEPT];
+    __shared__ int sm_sum[WARPS], sm_start, sm_item, sm_rows[LENGTHS], sm_pre[LENGTHS];
+    __shared__ float sm_ml[WARPS][HEADS][2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     if (threadIdx.x == 0) {
         for (int w = 0; w < WARPS; ++w)
@@ -100,12 +104,15 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
 
     // ---- this block's share, by a prefix sum over the items
     // (in 32 bits: the host has seen to it)
-    const bool kept = a.items <= KEPT;
+    const bool kept = !ALONE && a.items <= KEPT;
     auto own_of = [&](int item) { return a.k.table ? a.k.rows_of(item / a.HG) : 0; };
     auto pre_of = [&](int item) { return a.fold.rows ? a.fold.rows_of(item / a.HG % a.fold.heads) : 0; };
     auto rows_of = [&](int item) { return kept ? sm_rows[item] : own_of(item); };
     auto prefix_of = [&](int item) { return kept ? sm_pre[item] : pre_of(item); };
     auto blocks_of = [&](int item) { return ((rows_of(item) + 15) >> 4) + ((prefix_of(item) + 15) >> 4); };
+    bool busy = true;
+    int q = 0, f0 = 0, f1 = 0;
+    if constexpr (!ALONE) {
     const int E = (a.items + NT - 1) / NT, i0 = min(a.items, (int)threadIdx.x * E), i1 = min(a.items, i0 + E);
     int mine = 0;
     for (int i = i0; i < i1; ++i) {
@@ -131,9 +138,11 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // (beside a prefix these blocks have the SMs that it leaves; the other blocks have nothing to do)
     int ctas = gridDim.x;
     if (a.pre.units) ctas = min(ctas, PER_SM * (SMS - prefix_sms(block_sum<NT>(a.pre.part(NT), sm_all), total, D)));
-    const int warps = ctas * WARPS, q = max((total + warps - 1) / warps, MIN_BLOCKS);
-    const int f0 = (int)min((long long)total, (long long)blockIdx.x * WARPS * q), f1 = (int)min((long long)total, (long long)f0 + WARPS * q);
-    const bool busy = (int)blockIdx.x < ctas && f0 < f1;
+    const int warps = ctas * WARPS;
+    q = max((total + warps - 1) / warps, MIN_BLOCKS);
+    f0 = (int)min((long long)total, (long long)blockIdx.x * WARPS * q);
+    f1 = (int)min((long long)total, (long long)f0 + WARPS * q);
+    busy = (int)blockIdx.x < ctas && f0 < f1;
     if (busy && before <= f0 && f0 < before + mine) {                  // true in exactly one thread
         int st = before, id = i0;
         for (;; ++id) {
@@ -145,25 +154,37 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         sm_item = id;
     }
     __syncthreads();
+    }
     if (busy) {
         // ---- this warp's share
-        int start = sm_start;                       // blocks before the cursor's item
         Cursor cur;
-        const int w0 = min(f1, f0 + warp * q), w1 = min(f1, w0 + q);
         auto settle = [&](Cursor& c) {
             c.n = rows_of(c.item);
             c.np = prefix_of(c.item);
             c.blocks = ((c.n + 15) >> 4) + ((c.np + 15) >> 4);
         };
-        cur.item = sm_item;
-        settle(cur);
-        cur.left = w1 - w0;
-        while (cur.left > 0 && start + cur.blocks <= w0) {
-            start += cur.blocks;
-            ++cur.item;
+        int w1;                                     // where this warp's share ends
+        if constexpr (ALONE) {
+            cur.item = blockIdx.x;
             settle(cur);
+            cur.b = cur.blocks * warp / WARPS;
+            w1 = cur.blocks * (warp + 1) / WARPS;
+            cur.left = w1 - cur.b;
+        } else {
+            int start = sm_start;                   // blocks before the cursor's item
+            const int w0 = min(f1, f0 + warp * q);
+            w1 = min(f1, w0 + q);
+            cur.item = sm_item;
+            settle(cur);
+            cur.left = w1 - w0;
+            while (cur.left > 0 && start + cur.blocks <= w0) {
+                start += cur.blocks;
+                ++cur.item;
+                settle(cur);
+            }
+            cur.b = w0 - start;
         }
-        cur.b = w0 - start;
+        [[maybe_unused]] const int share = cur.left;
         auto advance = [&](Cursor c) {
             if (--c.left > 0 && ++c.b == c.blocks) {
                 c.b = 0;
@@ -199,7 +220,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (c.left <= 0 || lane != 0) return;
             uint64_t* bar = &full[warp][s];
 #ifdef KVM_TEST_DROP_ATTEND_STAGE
-            if (blockIdx.x == KVM_TEST_DROP_CTA && warp == 0 && c.left == w1 - w0 - (KVM_TEST_DROP_ATTEND_STAGE)) return;   // test build only: this block never arrives
+            if (blockIdx.x == KVM_TEST_DROP_CTA && warp == 0 && c.left == share - (KVM_TEST_DROP_ATTEND_STAGE)) return;   // test build only: this block never arrives
 #endif
             if (!exists(c, page)) {
                 mbar_arrive(bar);
@@ -313,6 +334,18 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     for (int z = 4; z < 32; z <<= 1) l[y] += __shfl_xor_sync(0xffffffffu, l[y], z);
                     if (!ok) l[y] = NAN;
                 }
+                if constexpr (ALONE) {                   // (all of the warp's copies have been used: the ring's memory takes the state)
+                    float* so = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                        for (int j = 0; j < MT; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) so[(2 * tig + y) * D + j * 16 + e * 8 + gid] = o[j][2 * e + y];
+                        if (gid == 0) { sm_ml[warp][2 * tig + y][0] = m[y]; sm_ml[warp][2 * tig + y][1] = l[y]; }
+                    }
+                    break;
+                }
                 const int w = blockIdx.x * WARPS + warp;
                 if (b_first == 0 && lane == 0) {
                     // parts after the first one begin at the next warps' shares
@@ -347,6 +380,30 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             cur = nxt;
             s = s + 1 == STAGES ? 0 : s + 1;
         }
+        if constexpr (ALONE) {
+            if (share == 0 && lane < HEADS) { sm_ml[warp][lane][0] = LOWEST; sm_ml[warp][lane][1] = 0.f; }
+            __syncthreads();
+            const int item = blockIdx.x, u = item / a.HG, h0 = (item - u * a.HG) * HEADS, heads = min(a.G - h0, HEADS);
+            const float* all = reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw)) - warp * RING_BYTES);
+            for (int i = threadIdx.x; i < heads * D / 2; i += NT) {
+                const int h = i / (D / 2), c = i % (D / 2) * 2;
+                float M = LOWEST, L = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+                for (int x = 0; x < WARPS; ++x) M = fmaxf(M, sm_ml[x][h][0]);
+#pragma unroll
+                for (int x = 0; x < WARPS; ++x) {
+                    if (sm_ml[x][h][1] == 0.f) continue;          // (a warp without rows)
+                    const float f = ex2(sm_ml[x][h][0] - M);
+                    const float2 v = *reinterpret_cast<const float2*>(all + x * (RING_BYTES / 4) + h * D + c);
+                    L = fmaf(sm_ml[x][h][1], f, L);
+                    y0 = fmaf(v.x, f, y0);
+                    y1 = fmaf(v.y, f, y1);
+                }
+                const float f = L == 0.f ? 0.f : 1.f / L;
+                *reinterpret_cast<uint32_t*>(a.out + ((size_t)u * a.G + h0 + h) * D + c) =
+                    Vec<__nv_bfloat16>::pack2(f != 0.f ? y0 * f : 0.f, f != 0.f ? y1 * f : 0.f);
+            }
+        }
         if (!ok) {
             // copies in flight land before shared memory is given back (bounded)
             if (a.stats) a.stats->status = KVM_E_DEVICE_TIMEOUT;
@@ -370,7 +427,7 @@ bool make_pool_map(CUtensorMap* map, const void* ptr, long long rows, int D) {
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cudaStream_t st) {
+template <int D, bool ALONE> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cudaStream_t st) {
     constexpr size_t smem = 1024 + WARPS * RING_BYTES;
     static std::mutex mu;
     static bool ready[KVM_MAX_DEVICES] = {};
@@ -381,7 +438,7 @@ template <int D> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cuda
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev]) {
-            if ((e = cudaFuncSetAttribute(rows_paged_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+            if ((e = cudaFuncSetAttribute(rows_paged_kernel<D, ALONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
             ready[dev] = true;
         }
     }
@@ -391,10 +448,16 @@ template <int D> cudaError_t launch_t(const PagedPlan& plan, const Args& a, cuda
     if (prefix && (!make_pool_map(&pk, a.fold.K, prefix, D) || !make_pool_map(&pv, a.fold.V, prefix, D))) return cudaErrorNotSupported;
     if (!a.k.table) { mk = pk; mv = pv; }           // (never read from)
     if (!prefix) { pk = mk; pv = mv; }
-    return launch_dependent(rows_paged_kernel<D>, dim3(plan.grid), dim3(NT), smem, st, mk, mv, pk, pv, a);
+    return launch_dependent(rows_paged_kernel<D, ALONE>, dim3(plan.grid), dim3(NT), smem, st, mk, mv, pk, pv, a);
 }
 
 }  // namespace
+
+// A block per unit where its four warps are not long at it: nothing is joined by a second kernel.  (us, shares / alone, lengths in the upper half of
+// `rows`, 128 channels: 32 units x 256 rows 9.9 / 6.5, x 512 11.2 / 10.1, x 1024 11.0 / 17.3; 128 x 256 11.6 / 6.6, x 1024 19.4 / 18.6, x 2048 26.3 /
+// 32.9; 256 x 512 18.5 / 13.7, x 1024 25.7 / 22.3; 512 x 512 27.3 / 24.1; 768 x 256 25.3 / 22.9.  64 channels: 32 x 512 9.7 / 8.6, 128 x 1024 14.1 /
+// 15.0, 256 x 1024 20.4 / 17.5.)
+static bool alone(int items, int rows) { return items <= 6 * SMS && (rows <= 512 || (items > SMS && rows <= 1024)); }
 
 // (148 SMs; as many blocks as a share of MIN_BLOCKS per warp needs at most.)
 PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix) {
@@ -404,6 +467,8 @@ PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix) {
     const long long most = ((long long)p.items * ((rows + 15) / 16) + MIN_BLOCKS * WARPS - 1) / (MIN_BLOCKS * WARPS);
     const int sms = beside_prefix ? OWN_MOST : SMS;
     p.grid = (int)(most < PER_SM * sms ? most : PER_SM * sms);
+    p.alone = !beside_prefix && alone(p.items, rows);
+    if (p.alone) p.grid = p.items;
     p.slots = p.items + p.grid * WARPS + 1;
     p.slot_rows = s.G < HEADS ? s.G : HEADS;
     return p;
@@ -412,7 +477,8 @@ PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix) {
 cudaError_t launch_rows_paged(const Shape& s, const PagedPlan& plan, const void* q, const Keys& k, const Fold& fold, const Beside& pre, const States& states, void* out,
                               kvm_stats* stats, cudaStream_t st) {
     const Args a = {(const __nv_bfloat16*)q, k, fold, states, pre, (__nv_bfloat16*)out, stats, s.G, plan.hg, plan.items, s.scale * LOG2E};
-    return s.D == 128 ? launch_t<128>(plan, a, st) : launch_t<64>(plan, a, st);
+    return plan.alone ? (s.D == 128 ? launch_t<128, true>(plan, a, st) : launch_t<64, true>(plan, a, st))
+                      : (s.D == 128 ? launch_t<128, false>(plan, a, st) : launch_t<64, false>(plan, a, st));
 }
 
 }  // namespace serve

@@ -189,7 +189,7 @@ cudaError_t launch_rows_tc(const Shape& s, const TcPlan& plan, int units, const 
 
 // Decode attention over a paged cache (bf16), one query per sequence: rows_paged.cu.
 struct PagedPlan {
-    int hg, items, grid, slot_rows;             // groups of up to 8 heads per unit; items = units x groups
+    int hg, items, grid, slot_rows, alone;      // groups of up to 8 heads per unit; items = units x groups; alone: a block per item, nothing to join
     long long slots;
 };
 PagedPlan paged_plan(const Shape& s, int rows, bool beside_prefix);

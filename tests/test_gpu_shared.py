@@ -81,6 +81,9 @@ SHAPES = [
     (5, 40, 2, 64, 260, 50, 16),           # blocks of twenty rows
     (2, 136, 1, 128, 150, 20, 16),         # a block of more than 128 rows
     (9, 3, 3, 128, 1000, 100, 64),
+    (2, 4, 4, 128, 0, 1500, 16),           # units in parts
+    (40, 8, 8, 64, 0, 700, 32),            # a block per unit, and some
+    (50, 18, 18, 64, 0, 20, 16),           # more units than blocks at a time
     (20, 64, 16, 64, 2500, 10, 16),        # more steps over the prefix than SMs
 ]
 

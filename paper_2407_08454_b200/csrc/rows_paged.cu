@@ -61,11 +61,6 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y) : "memory");
-}
-
 // Where a warp stands in the list of blocks.
 struct Cursor {
     int item, b, blocks, n, np;             // block b of `blocks` of item's unit, which has n rows of its own, behind np of a folded prefix
@@ -105,8 +100,9 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // ---- this block's share, by a prefix sum over the items
     // (in 32 bits: the host has seen to it)
     const bool kept = !ALONE && a.items <= KEPT;
-    auto own_of = [&](int item) { return a.k.table ? a.k.rows_of(item / a.HG) : 0; };
-    auto pre_of = [&](int item) { return a.fold.rows ? a.fold.rows_of(item / a.HG % a.fold.heads) : 0; };
+    auto unit_of = [&](int item) { return a.HG == 1 ? item : item / a.HG; };
+    auto own_of = [&](int item) { return a.k.table ? a.k.rows_of(unit_of(item)) : 0; };
+    auto pre_of = [&](int item) { return a.fold.rows ? a.fold.rows_of(unit_of(item) % a.fold.heads) : 0; };
     auto rows_of = [&](int item) { return kept ? sm_rows[item] : own_of(item); };
     auto prefix_of = [&](int item) { return kept ? sm_pre[item] : pre_of(item); };
     auto blocks_of = [&](int item) { return ((rows_of(item) + 15) >> 4) + ((prefix_of(item) + 15) >> 4); };
@@ -199,15 +195,16 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // of a block of own rows its page, of one of the folded prefix its first row in the prefix's tensor
         auto page_of = [&](const Cursor& c) {
             if (c.left <= 0) return -1;
-            const int u = c.item / a.HG, b = c.b - ((c.np + 15) >> 4);
+            const int u = unit_of(c.item), b = c.b - ((c.np + 15) >> 4);
             return b < 0 ? u % a.fold.heads * a.fold.rows + c.b * 16 : __ldg(a.k.table + (size_t)u * a.k.max_pages + (b >> bshift));
         };
         auto folded = [&](const Cursor& c) { return c.b < ((c.np + 15) >> 4); };
         auto exists = [&](const Cursor& c, int page) { return folded(c) || (unsigned)page < (unsigned)a.k.n_pages; };
         const uint32_t ring = ((smem_u32(smem_raw) + 1023u) & ~1023u) + warp * RING_BYTES;
+        uint8_t* ring_at = smem_raw + (ring - smem_u32(smem_raw));
         uint32_t qf[D / 16][2];                     // q^T as the second operand: channels 2 tig.. (+ 8) of head gid
         auto load_q = [&](const Cursor& c) {
-            const int u = c.item / a.HG, h = (c.item - u * a.HG) * HEADS + gid;
+            const int u = unit_of(c.item), h = (c.item - u * a.HG) * HEADS + gid;
             const uint32_t* p = reinterpret_cast<const uint32_t*>(a.q + ((size_t)u * a.G + h) * D) + tig;
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
@@ -230,11 +227,9 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const bool pre = folded(c);
             const int row = pre ? page : (page << a.k.shift) + (((c.b - ((c.np + 15) >> 4)) & bmask) << 4);
             const CUtensorMap *mk = pre ? &map_pk : &map_k, *mv = pre ? &map_pv : &map_v;
-#pragma unroll
-            for (int i = 0; i < KCH; ++i) {
-                tma_load_2d(ring + s * STAGE + i * CHUNK, mk, bar, i * 64, row);
-                tma_load_2d(ring + s * STAGE + TENSOR + i * CHUNK, mv, bar, i * 64, row);
-            }
+            // (both column chunks in one copy: the thread that issues is one of those that compute)
+            tma_load_3d(ring_at + s * STAGE, mk, bar, 0, row, 0);
+            tma_load_3d(ring_at + s * STAGE + TENSOR, mv, bar, 0, row, 0);
         };
         float o[MT][4];                             // channels of product j: 16 j + gid (+ 8), heads 2 tig, 2 tig + 1
         float m[2], l[2];
@@ -326,7 +321,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             __syncwarp();                           // (all lanes have read the stage)
             if (ok) copy_next(s);
             if (last) {                             // the part's end: its state, or the output
-                const int u = cur.item / a.HG, h0 = (cur.item - u * a.HG) * HEADS;
+                const int u = unit_of(cur.item), h0 = (cur.item - u * a.HG) * HEADS;
                 const bool whole = b_first == 0 && cur.b == cur.blocks - 1;
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
@@ -335,7 +330,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     if (!ok) l[y] = NAN;
                 }
                 if constexpr (ALONE) {                   // (all of the warp's copies have been used: the ring's memory takes the state)
-                    float* so = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+                    float* so = reinterpret_cast<float*>(ring_at);
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
 #pragma unroll
@@ -384,7 +379,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             if (share == 0 && lane < HEADS) { sm_ml[warp][lane][0] = LOWEST; sm_ml[warp][lane][1] = 0.f; }
             __syncthreads();
             const int item = blockIdx.x, u = item / a.HG, h0 = (item - u * a.HG) * HEADS, heads = min(a.G - h0, HEADS);
-            const float* all = reinterpret_cast<const float*>(smem_raw + (ring - smem_u32(smem_raw)) - warp * RING_BYTES);
+            const float* all = reinterpret_cast<const float*>(ring_at - warp * RING_BYTES);
             for (int i = threadIdx.x; i < heads * D / 2; i += NT) {
                 const int h = i / (D / 2), c = i % (D / 2) * 2;
                 float M = LOWEST, L = 0.f, y0 = 0.f, y1 = 0.f;
@@ -415,15 +410,16 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (a.pre.units) grid_dependency_wait();        // (who joins waits for this kernel, and thereby for the prefix's)
 }
 
-// Rows (all pages', or a prefix's of all heads) as a tensor [rows, D], boxes of [16 rows, 64 channels].
+// Rows (all pages', or a prefix's of all heads) as a tensor [D / 64, rows, 64], boxes of [all, 16 rows, 64 channels]: the column chunks of 16 rows
+// one after the other.
 bool make_pool_map(CUtensorMap* map, const void* ptr, long long rows, int D) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)D * 2};
-    cuuint32_t box[2] = {64, STAGE_ROWS};
-    cuuint32_t estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(D / 64)};
+    cuuint64_t strides[2] = {(cuuint64_t)D * 2, 128};
+    cuuint32_t box[3] = {64, STAGE_ROWS, (cuuint32_t)(D / 64)};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -454,7 +450,7 @@ template <int D, bool ALONE> cudaError_t launch_t(const PagedPlan& plan, const A
 }  // namespace
 
 // A block per unit where its four warps are not long at it: nothing is joined by a second kernel.  (us, shares / alone, lengths in the upper half of
-// `rows`, 128 channels: 32 units x 256 rows 9.9 / 6.5, x 512 11.2 / 10.1, x 1024 11.0 / 17.3; 128 x 256 11.6 / 6.6, x 1024 19.4 / 18.6, x 2048 26.3 /
+// `rows`, 128 channels: 32 units x 256 rows 9.9 / 6.0, x 512 11.2 / 9.0, x 1024 11.0 / 17.3; 128 x 256 11.6 / 5.9, x 1024 19.4 / 18.6, x 2048 26.3 /
 // 32.9; 256 x 512 18.5 / 13.7, x 1024 25.7 / 22.3; 512 x 512 27.3 / 24.1; 768 x 256 25.3 / 22.9.  64 channels: 32 x 512 9.7 / 8.6, 128 x 1024 14.1 /
 // 15.0, 256 x 1024 20.4 / 17.5.)
 static bool alone(int items, int rows) { return items <= 6 * SMS && (rows <= 512 || (items > SMS && rows <= 1024)); }

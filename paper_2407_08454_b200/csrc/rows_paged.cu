@@ -108,48 +108,50 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     auto blocks_of = [&](int item) { return ((rows_of(item) + 15) >> 4) + ((prefix_of(item) + 15) >> 4); };
     bool busy = true;
     int q = 0, f0 = 0, f1 = 0;
-    if constexpr (!ALONE) {
-    const int E = (a.items + NT - 1) / NT, i0 = min(a.items, (int)threadIdx.x * E), i1 = min(a.items, i0 + E);
-    int mine = 0;
-    for (int i = i0; i < i1; ++i) {
-        const int n = own_of(i), np = pre_of(i);
-        if (kept) { sm_rows[i] = n; sm_pre[i] = np; }
-        mine += ((n + 15) >> 4) + ((np + 15) >> 4);
-        if (blockIdx.x == 0 && n + np == 0) a.st.pieces[i] = make_int4(0, 0, 0, 0);
-    }
-    int inc = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-    }
-    if (lane == 31) sm_sum[warp] = inc;
-    __syncthreads();
-    int total = 0, before = inc - mine;
-#pragma unroll
-    for (int x = 0; x < WARPS; ++x) {
-        if (x < warp) before += sm_sum[x];
-        total += sm_sum[x];
-    }
-    // (beside a prefix these blocks have the SMs that it leaves; the other blocks have nothing to do)
-    int ctas = gridDim.x;
-    if (a.pre.units) ctas = min(ctas, PER_SM * (SMS - prefix_sms(block_sum<NT>(a.pre.part(NT), sm_all), total, D)));
-    const int warps = ctas * WARPS;
-    q = max((total + warps - 1) / warps, MIN_BLOCKS);
-    f0 = (int)min((long long)total, (long long)blockIdx.x * WARPS * q);
-    f1 = (int)min((long long)total, (long long)f0 + WARPS * q);
-    busy = (int)blockIdx.x < ctas && f0 < f1;
-    if (busy && before <= f0 && f0 < before + mine) {                  // true in exactly one thread
-        int st = before, id = i0;
-        for (;; ++id) {
-            const int n = blocks_of(id);
-            if (st + n > f0) break;
-            st += n;
+    if constexpr (ALONE) {
+        __syncthreads();                            // (the barriers are there)
+    } else {
+        const int E = (a.items + NT - 1) / NT, i0 = min(a.items, (int)threadIdx.x * E), i1 = min(a.items, i0 + E);
+        int mine = 0;
+        for (int i = i0; i < i1; ++i) {
+            const int n = own_of(i), np = pre_of(i);
+            if (kept) { sm_rows[i] = n; sm_pre[i] = np; }
+            mine += ((n + 15) >> 4) + ((np + 15) >> 4);
+            if (blockIdx.x == 0 && n + np == 0) a.st.pieces[i] = make_int4(0, 0, 0, 0);
         }
-        sm_start = st;
-        sm_item = id;
-    }
-    __syncthreads();
+        int inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
+        }
+        if (lane == 31) sm_sum[warp] = inc;
+        __syncthreads();
+        int total = 0, before = inc - mine;
+#pragma unroll
+        for (int x = 0; x < WARPS; ++x) {
+            if (x < warp) before += sm_sum[x];
+            total += sm_sum[x];
+        }
+        // (beside a prefix these blocks have the SMs that it leaves; the other blocks have nothing to do)
+        int ctas = gridDim.x;
+        if (a.pre.units) ctas = min(ctas, PER_SM * (SMS - prefix_sms(block_sum<NT>(a.pre.part(NT), sm_all), total, D)));
+        const int warps = ctas * WARPS;
+        q = max((total + warps - 1) / warps, MIN_BLOCKS);
+        f0 = (int)min((long long)total, (long long)blockIdx.x * WARPS * q);
+        f1 = (int)min((long long)total, (long long)f0 + WARPS * q);
+        busy = (int)blockIdx.x < ctas && f0 < f1;
+        if (busy && before <= f0 && f0 < before + mine) {                  // true in exactly one thread
+            int st = before, id = i0;
+            for (;; ++id) {
+                const int n = blocks_of(id);
+                if (st + n > f0) break;
+                st += n;
+            }
+            sm_start = st;
+            sm_item = id;
+        }
+        __syncthreads();
     }
     if (busy) {
         // ---- this warp's share

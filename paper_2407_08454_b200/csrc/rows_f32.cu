@@ -84,25 +84,36 @@ template <typename T, int D, int MT, int NT> __device__ __forceinline__ void loa
     }
 }
 
-// E neighbouring channels of a finished row from channel c: to the output, or to the piece's state.
-template <typename T, int D, int E>
-__device__ __forceinline__ void finish(const Args& a, int u, int item, int piece, int row, int m_row, int c, const float* o, float m, float l) {
-    if (a.pieces > 1 || a.st.o) {
-        const size_t r = (((size_t)u * a.st.items + item) * a.pieces + piece) * a.st.rows + row;
+// A finished row on its way to the output, or to the piece's state.  The lanes that hold its channels each work out the row's end once; then, a
+// __syncwarp() later, they put their channels and one of them the sums: lse_in may be lse, so nobody may read it after that.
+template <typename T, int D> struct RowTo {
+    const Args& a;
+    bool state;
+    size_t at;                              // row of the states or of the output
+    float m, l;
+    RowEnd end;
+    // (live: a row of the unit; of those past its last one nothing is read)
+    __device__ __forceinline__ RowTo(const Args& args, int u, int item, int piece, int row, int m_row, bool live, float m0, float l0)
+        : a(args), state(args.pieces > 1 || args.st.o),
+          at(state ? (((size_t)u * args.st.items + item) * args.pieces + piece) * args.st.rows + row : (size_t)args.q.at(u, m_row)), m(m0), l(l0),
+          end(m0, l0, l0, live && !state ? args.out.lse_in : nullptr, at) {}
+    // E neighbouring channels from channel c
+    template <int E> __device__ __forceinline__ void channels(int c, const float* o) const {
 #pragma unroll
-        for (int e = 0; e < E; ++e) a.st.o[r * D + c + e] = o[e];
-        if (c == 0) a.st.ml[r] = make_float4(m, l, l, 0.f);
-        return;
+        for (int e = 0; e < E; ++e) {
+            if (state) {
+                a.st.o[at * D + c + e] = o[e];
+            } else {
+                const float x = a.out.O_in ? (float)((const T*)a.out.O_in)[at * D + c + e] : 0.f;
+                ((T*)a.out.O)[at * D + c + e] = (T)end_value(o[e], end.f, x, end.f_in);
+            }
+        }
     }
-    const long long at = a.q.at(u, m_row);
-    const RowEnd end(m, l, l, a.out.lse_in, at);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float x = a.out.O_in ? (float)((const T*)a.out.O_in)[at * D + c + e] : 0.f;
-        ((T*)a.out.O)[at * D + c + e] = (T)end_value(o[e], end.f, x, end.f_in);
+    __device__ __forceinline__ void sums() const {
+        if (state) a.st.ml[at] = make_float4(m, l, l, 0.f);
+        else if (a.out.lse) a.out.lse[at] = end.lse;
     }
-    if (c == 0 && a.out.lse) a.out.lse[at] = end.lse;
-}
+};
 
 // This block's keys: the piece's share of the unit's tiles.
 template <int KT> __device__ __forceinline__ void share(const Args& a, int u, int& r0, int& r1) {
@@ -190,7 +201,10 @@ template <typename T, int D> __global__ void __launch_bounds__(NT8) rows8_kernel
             if (m0 + row >= a.q.rows()) break;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[i][e] += sk[row * P + lane * E + e];
-            finish<T, D, E>(a, u, blockIdx.x, blockIdx.y, row, m0 + row, lane * E, o[i], sp[row][0], sp[row][1]);
+            const RowTo<T, D> to(a, u, blockIdx.x, blockIdx.y, row, m0 + row, true, sp[row][0], sp[row][1]);
+            __syncwarp();
+            to.template channels<E>(lane * E, o[i]);
+            if (lane == 0) to.sums();
         }
 }
 
@@ -366,9 +380,13 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
         const int row = warp * 16 + gid + h * 8, mr = blockIdx.x * MT + row;
-        if (mr >= a.q.rows()) continue;
+        const bool live = mr < a.q.rows();
+        const RowTo<float, D> to(a, u, blockIdx.x, blockIdx.y, row, mr, live, m[h], l[h]);
+        __syncwarp();
+        if (!live) continue;
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j) finish<float, D, 2>(a, u, blockIdx.x, blockIdx.y, row, mr, j * 8 + 2 * tig, &o[j][2 * h], m[h], l[h]);
+        for (int j = 0; j < D / 8; ++j) to.template channels<2>(j * 8 + 2 * tig, &o[j][2 * h]);
+        if (tig == 0) to.sums();
     }
 }
 

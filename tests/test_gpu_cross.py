@@ -117,3 +117,20 @@ def test_a_maximum_that_keeps_growing(dtype):
         ref = Rows(Q[0, h], K[0, h], V[0, h], 1.0 / math.sqrt(D))
         close(O[0, h], ref.O, ref.O_bound(dtype), h)
         close(lse[0, h], ref.lse, ref.lse_bound(), h)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n_q,rows,D", [
+    (2, 8, 4, 20, 100, 64),               # the rows of a unit in one tile, its keys in one piece
+    (2, 8, 4, 20, 128, 128),
+    (1, 2, 1, 45, 1, 128),                # a tile and a bit
+    (37, 8, 8, 64, 300, 128),             # as many blocks as run at a time: longer caches stay in one piece
+    (37, 12, 12, 40, 260, 64),
+    (5, 8, 8, 3, 120, 128),               # few rows
+    (3, 8, 2, 4, 90, 64),
+])
+def test_fp32_in_place_with_the_keys_in_one_piece(B, Hq, Hkv, n_q, rows, D):
+    """Nothing is joined by a second kernel: the one that attends reads O_in and lse_in and overwrites them."""
+    p = kvm.make_params(B, Hq, Hkv, 1, D, torch.float32)
+    assert kvm.kvm_cross_workspace_bytes(p, n_q, rows) <= 256          # no states
+    for lengths in ("ragged", None):
+        check(B, Hq, Hkv, n_q, rows, D, torch.float32, join=True, in_place=True, lengths=lengths)

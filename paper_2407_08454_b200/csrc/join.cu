@@ -135,7 +135,7 @@ template <int D> __device__ __forceinline__ void join_warps(Sum<D / 32>& s) {
     s.m = M;
 }
 
-// The row's sums to the output (row w).
+// The row's sums to the output (row w), by a whole warp.
 template <typename T, int D> __device__ __forceinline__ void store_row(const Sum<D / 32>& s, const Output& out, long long w) {
     constexpr int E = D / 32;
     const int lane = threadIdx.x & 31;
@@ -156,6 +156,7 @@ template <typename T, int D> __device__ __forceinline__ void store_row(const Sum
 #pragma unroll
         for (int e = 0; e < E; ++e) orow[e] = (T)y[e];
     }
+    __syncwarp();                               // (all lanes have read lse_in, which may be lse)
     if (out.lse && lane == 0) out.lse[w] = end.lse;
 }
 

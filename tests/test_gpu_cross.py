@@ -134,3 +134,13 @@ def test_fp32_in_place_with_the_keys_in_one_piece(B, Hq, Hkv, n_q, rows, D):
     assert kvm.kvm_cross_workspace_bytes(p, n_q, rows) <= 256          # no states
     for lengths in ("ragged", None):
         check(B, Hq, Hkv, n_q, rows, D, torch.float32, join=True, in_place=True, lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,Hq,Hkv,n_q,rows,D", [
+    (1, 4, 2, 60, 3000, 128),             # few items in many pieces: a block joins a row
+    (3, 4, 4, 300, 4000, 64),             # a warp for each of a block's four rows
+    (13, 16, 16, 150, 2700, 64),          # many items: sixteen rows a block
+])
+def test_in_place_joined_by_a_second_kernel(B, Hq, Hkv, n_q, rows, D, dtype):
+    check(B, Hq, Hkv, n_q, rows, D, dtype, join=True, in_place=True)

@@ -90,7 +90,7 @@ struct Output {
 __device__ __forceinline__ float rescale2(float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); }
 
 // One row's result from its sums, N channels at a time: o / lr, joined with O_in under both log-sum-exps.
-// (l = 0: no keys.  NaN sums stay NaN.)
+// (l = 0: no keys, the row is what is joined in, bit for bit.  NaN sums, and a NaN lse_in, are the mark of a wait that gave up, and stay.)
 struct RowEnd {
     float f, f_in, lse;
     __device__ __forceinline__ RowEnd(float m, float l, float lr, const float* lse_in, long long row) {
@@ -99,8 +99,14 @@ struct RowEnd {
         f_in = 0.f;
         lse = none ? -INFINITY : (m + log2f(l)) * LN2;
         if (lse_in) {
-            const float z = lse_in[row], M = fmaxf(lse, z);
-            if (M == -INFINITY) { lse = M; return; }             // neither has keys
+            const float z = lse_in[row];
+            if (none) {
+                f_in = z == -INFINITY ? 0.f : 1.f;
+                lse = z;
+                return;
+            }
+            if (z == -INFINITY) return;                          // nothing to join
+            const float M = fmaxf(lse, z);
             const float a = expf(lse - M), b = expf(z - M), s = a + b;
             f *= a / s;
             f_in = b / s;

@@ -144,3 +144,40 @@ def test_fp32_in_place_with_the_keys_in_one_piece(B, Hq, Hkv, n_q, rows, D):
 ])
 def test_in_place_joined_by_a_second_kernel(B, Hq, Hkv, n_q, rows, D, dtype):
     check(B, Hq, Hkv, n_q, rows, D, dtype, join=True, in_place=True)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n_q,rows,D,dtype", [
+    (1, 4, 2, 40, 300, 128, torch.bfloat16),      # items stay whole
+    (1, 4, 2, 150, 6000, 128, torch.bfloat16),    # items are cut
+    (1, 5, 5, 9, 24000, 64, torch.bfloat16),      # two states to a piece
+    (1, 4, 2, 40, 100, 64, torch.float32),        # one piece, several; few rows the same
+    (1, 4, 2, 40, 3000, 128, torch.float32),
+    (1, 4, 2, 3, 100, 64, torch.float32),
+    (1, 4, 2, 3, 3000, 64, torch.float32),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_a_mark_of_what_gave_up_stays(B, Hq, Hkv, n_q, rows, D, dtype, in_place):
+    """lse_in is NaN where the attention that is joined in gave up: so are O and lse then, and a unit without keys passes both on as they are."""
+    g = torch.Generator().manual_seed(41)
+    G = Hq // Hkv
+    p = kvm.make_params(B, Hq, Hkv, 1, D, dtype)
+    Q = torch.randn(B, Hq, n_q, D, generator=g).to(dtype)
+    K, V = (torch.randn(B, Hkv, rows, D, generator=g).to(dtype) for _ in range(2))
+    ln = torch.full((B, Hkv), rows, dtype=torch.int32)
+    ln[0, 0] = 0
+    O_in, lse_in = torch.randn(B, Hq, n_q, D, generator=g).to(dtype), math.log(rows) + torch.randn(B, Hq, n_q, generator=g)
+    lse_in[:, :, :2] = math.nan
+    O_in[:, :, 0] = math.nan
+    a, b = O_in.cuda(), lse_in.cuda()
+    O, lse = (a, b) if in_place else (torch.zeros_like(a), torch.zeros_like(b))
+    ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n_q, rows), dtype=torch.uint8, device="cuda")
+    kvm.kvm_cross_attend(p, Q.cuda(), K.cuda(), V.cuda(), ln.cuda(), O, lse, ws, O_in=a, lse_in=b)
+    O, lse = O.cpu(), lse.cpu()
+    for h in range(Hq):
+        if h < G:
+            assert torch.equal(O[0, h].nan_to_num(7.0), O_in[0, h].nan_to_num(7.0)) and torch.equal(lse[0, h].nan_to_num(7.0), lse_in[0, h].nan_to_num(7.0))
+        else:
+            assert O[0, h, :2].isnan().all() and lse[0, h, :2].isnan().all()
+            ref = Rows(Q[0, h], K[0, h // G], V[0, h // G], 1.0 / math.sqrt(D)).joined(O_in[0, h], lse_in[0, h])
+            close(O[0, h, 2:], ref.O[2:], ref.O_bound(dtype)[2:], h)
+            close(lse[0, h, 2:], ref.lse[2:], ref.lse_bound()[2:], h)

@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
     const long long tokens = (long long)a.B * a.T, x = (long long)blockIdx.x * TPB + threadIdx.x / LPT;
     if (x >= tokens) return;                    // (leaving early counts as letting the next kernel lie ready)
     const int b = (int)(x / a.T), t = (int)(x % a.T);
+    const unsigned group = ((1u << LPT) - 1u) << (threadIdx.x % 32 / LPT * LPT);       // the token's lanes
     const int o0 = NEIGHBOURS ? lane * 2 * N : lane * N, o1 = NEIGHBOURS ? o0 + N : o0 + D / 2;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -105,8 +106,7 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
                     a.stats->status = KVM_E_PAGE;
                 }
             }
-            // (the token's lanes have all read the length: they are one warp's, and nothing above lets them drift apart for good)
-            __syncwarp(__activemask());
+            __syncwarp(group);                  // (the token's lanes have all read the length, which may be moved in place)
             if (a.len_out && t == 0 && lane == 0) a.len_out[u] = min(start[i] + cnt, a.c.room());
         }
     }

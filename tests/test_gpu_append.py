@@ -181,3 +181,29 @@ def test_offsets_past_32_bits():
     want = torch.cat([V[-1, :5], v[0, 0]]).double().mean(0)
     # weights of one seventh rounded to bf16 alike (they cancel against the rounded sum), fp32 sums, one rounding
     assert bool(((out[0, 0].double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.01 + 1e-5).all())
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,dtype", [
+    (2000, 32, 8, 128, torch.bfloat16), (1000, 32, 8, 128, torch.float32), (1900, 20, 20, 64, torch.bfloat16), (1600, 36, 36, 64, torch.float32),
+])
+def test_decode_steps_of_a_large_batch_with_lengths_in_place(B, Hq, Hkv, D, dtype):
+    """So many sequences that a block takes several heads of a token, a few at a time, and moves each one's length when its lanes have read it."""
+    g = torch.Generator(device="cuda").manual_seed(B)
+    U, R, room, steps = B * Hkv, 16, 2, 12
+    table = torch.randperm(U * room, generator=g, device="cuda").to(torch.int32).view(U, room)
+    pool = [torch.full((U * room, R, D), 7.0, dtype=dtype, device="cuda") for _ in range(2)]
+    want = [x.clone() for x in pool]
+    length = torch.randint(0, R * room - steps + 1, (U,), generator=g, device="cuda", dtype=torch.int32)
+    start = length.clone()
+    cache = kvm.make_pages(pool[0], pool[1], table, length)
+    p = kvm.make_params(B, Hq, Hkv, 1, D, dtype)
+    q = torch.randn(B, Hq, 1, D, generator=g, device="cuda").to(dtype)
+    q_out, units = torch.empty_like(q), torch.arange(U, device="cuda")
+    for s in range(steps):
+        k, v = (torch.randn(B, Hkv, 1, D, generator=g, device="cuda").to(dtype) for _ in range(2))
+        kvm.kvm_paged_append(p, cache, None, None, q, k, v, q_out, length)
+        rows = (start + s).long()
+        page = table[units, rows // R].long()
+        want[0][page, rows % R], want[1][page, rows % R] = k.view(U, D), v.view(U, D)
+        assert torch.equal(length, start + s + 1)
+    assert torch.equal(pool[0], want[0]) and torch.equal(pool[1], want[1]) and torch.equal(q_out, q)

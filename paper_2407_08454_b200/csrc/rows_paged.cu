@@ -136,7 +136,7 @@ rows_paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         // (beside a prefix these blocks have the SMs that it leaves; the other blocks have nothing to do)
         int ctas = gridDim.x;
         if (a.pre.units) ctas = min(ctas, PER_SM * (SMS - prefix_sms(block_sum<NT>(a.pre.part(NT), sm_all), total, D)));
-        const int warps = ctas * WARPS;
+        const int warps = max(ctas, 1) * WARPS;                            // (without own rows the prefix has all SMs)
         q = max((total + warps - 1) / warps, MIN_BLOCKS);
         f0 = (int)min((long long)total, (long long)blockIdx.x * WARPS * q);
         f1 = (int)min((long long)total, (long long)f0 + WARPS * q);

@@ -186,3 +186,22 @@ def test_lengths_outside_the_room_are_clamped():
         kvm.kvm_shared_attend(p, q, Kp, Vp, torch.tensor(pre_len, dtype=torch.int32, device="cuda"), own, out, ws)
         outs.append(out)
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,Hq,Hkv,D,prefix,held,R", [LARGE[0], LARGE[3], LARGE[6]])
+def test_a_large_batch_of_which_a_part_is_empty(B, Hq, Hkv, D, prefix, held, R, dtype):
+    """The first step behind a prompt has no own rows yet, beside a prefix with a kernel of its own; or nothing is in the prefix, or in either."""
+    own, pre = torch.zeros(B, Hkv, dtype=torch.int32), torch.zeros(Hkv, dtype=torch.int32)
+    check(B, Hq, Hkv, D, prefix, held, R, dtype, lengths=own)
+    check(B, Hq, Hkv, D, prefix, held, R, dtype, pre_len=pre)
+    check(B, Hq, Hkv, D, prefix, held, R, dtype, lengths=own, pre_len=pre)
+    own[B // 2, Hkv - 1] = 1                               # a single row
+    check(B, Hq, Hkv, D, prefix, held, R, dtype, lengths=own)
+    check(B, Hq, Hkv, D, prefix, held, R, dtype, lengths=own, pre_len=pre)
+
+
+@pytest.mark.parametrize("prefix", [0, 30, 200])           # none, one that is folded in, one with a kernel of its own
+def test_more_units_than_keep_their_lengths(prefix):
+    check(70, 16, 16, 64, prefix, 40, 16, torch.bfloat16)
+    check(70, 32, 16, 128, prefix, 600, 32, torch.bfloat16, lengths=torch.randint(0, 4, (70, 16), generator=torch.Generator().manual_seed(6), dtype=torch.int32) ** 3)

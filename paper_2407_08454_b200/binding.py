@@ -309,6 +309,18 @@ def _lengths(t: Optional[torch.Tensor], units: int, name: str, dev: int) -> Opti
     return t.data_ptr()
 
 
+_STATS_BYTES = ctypes.sizeof(KvmStats)
+
+
+def _memory(t: Optional[torch.Tensor], name: str, dev: int, least: int = 0) -> Optional[int]:
+    """Address of contiguous memory on the current device: a workspace, whose size the library checks, or `least` bytes."""
+    if t is None:
+        return None
+    if t.get_device() != dev or not t.is_contiguous() or t.nbytes < least:
+        raise ValueError(f"{name}: expected {least or 'contiguous'} bytes on the current CUDA device, got {t.nbytes} with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
 def rope_turns(head_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """The rotation's frequencies as kvm_paged_append takes them (kvm_rope_turns): int64 [head_dim / 2] on `device`."""
     host = torch.empty(max(1, head_dim // 2), dtype=torch.int64)
@@ -354,7 +366,8 @@ def kvm_paged_append(p: KvmParams, cache: KvmPages, pos, turns, q, k, v, q_out, 
     _call("kvm_paged_append", p, cache, _lengths(len_out, units, "len_out", dev), n, _lengths(new_len, units, "new_len", dev),
           _arg(pos, torch.int32, (B,), "pos", dev), _arg(turns, torch.int64, (D // 2,), "turns", dev),
           KVM_ROPE_NEIGHBOURS if interleaved else KVM_ROPE_HALVES, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(),
-          _STRIDES(*strides), _arg(q_out, dt, (B, Hq, n, D), "q_out", dev), _ptr(stats), _stream(stream))
+          _STRIDES(*strides), _arg(q_out, dt, (B, Hq, n, D), "q_out", dev),
+          _memory(stats, "stats", dev, _STATS_BYTES), _stream(stream))
 
 
 def kvm_shared_workspace_bytes(p: KvmParams, pre_rows: int, own: Optional[KvmPages]) -> int:
@@ -377,7 +390,8 @@ def kvm_shared_attend(p: KvmParams, q, K_pre, V_pre, pre_len, own: Optional[KvmP
     if own is not None:
         _check_pages(own, dev, B * Hkv, D, dt)
     _call("kvm_shared_attend", p, _arg(q, dt, (B, Hq, D), "q", dev), kp, vp, rows, _lengths(pre_len, Hkv, "pre_len", dev), own,
-          _arg(out, dt, (B, Hq, D), "out", dev), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
+          _arg(out, dt, (B, Hq, D), "out", dev), _memory(stats, "stats", dev, _STATS_BYTES), _memory(ws, "ws", dev),
+          0 if ws is None else ws.nbytes, _stream(stream))
 
 
 def kvm_cross_workspace_bytes(p: KvmParams, n_q: int, rows: int) -> int:
@@ -394,7 +408,8 @@ def kvm_cross_attend(p: KvmParams, Q, K, V, length, O, lse, ws, O_in=None, lse_i
     q_shape, k_shape, l_shape = (B, Hq, n, D), (B, Hkv, rows, D), (B, Hq, n)
     _call("kvm_cross_attend", p, _arg(Q, dt, q_shape, "Q", dev), n, _arg(K, dt, k_shape, "K", dev), _arg(V, dt, k_shape, "V", dev), rows,
           _lengths(length, B * Hkv, "length", dev), _arg(O_in, dt, q_shape, "O_in", dev), _arg(lse_in, torch.float32, l_shape, "lse_in", dev),
-          _arg(O, dt, q_shape, "O", dev), _arg(lse, torch.float32, l_shape, "lse", dev), _ptr(stats), _ptr(ws), ws.nbytes, _stream(stream))
+          _arg(O, dt, q_shape, "O", dev), _arg(lse, torch.float32, l_shape, "lse", dev), _memory(stats, "stats", dev, _STATS_BYTES), _memory(ws, "ws", dev),
+          0 if ws is None else ws.nbytes, _stream(stream))
 
 
 # ----------------------------------------------------------------------------- convenience

@@ -286,3 +286,16 @@ def test_rows_behind_the_outputs_are_left_as_they_were():
                 ws[-256:] = 99
                 kvm.kvm_shared_attend(p, q, Kp, Vp, None, None, out, ws[:-256])
                 assert (ob[:pad] == 7).all() and (ob[pad + out.numel():] == 7).all() and (ws[-256:] == 99).all()
+
+
+def test_workspaces_and_stats_on_the_host_are_refused():
+    p = kvm.make_params(1, 2, 2, 1, 64, torch.float32)
+    q, K, lse = torch.zeros(1, 2, 3, 64, device="cuda"), torch.zeros(1, 2, 5, 64, device="cuda"), torch.zeros(1, 2, 3, device="cuda")
+    ws = torch.zeros(kvm.kvm_cross_workspace_bytes(p, 3, 5), dtype=torch.uint8, device="cuda")
+    for w, stats in ((ws.cpu(), None), (ws, kvm.new_stats("cpu")), (ws, kvm.new_stats("cuda")[:-8])):
+        with pytest.raises(ValueError):
+            kvm.kvm_cross_attend(p, q, K, K, None, q.clone(), lse, w, stats=stats)
+        with pytest.raises(ValueError):
+            kvm.kvm_shared_attend(p, q[:, :, 0].contiguous(), K[0], K[0], None, None, q[:, :, 0].contiguous(), w, stats=stats)
+    with pytest.raises(kvm.KvmError):
+        kvm.kvm_cross_attend(p, q, K, K, None, q.clone(), lse, None)

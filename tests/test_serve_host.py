@@ -137,3 +137,43 @@ def test_the_binding_refuses_tensors_of_another_shape_type_or_device():
         kvm.make_pages(torch.zeros(4, 16, 64), torch.zeros(4, 16, 64), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
     assert "page" in kvm.status_string(kvm.KVM_E_PAGE)
     assert binding.KVM_E_PAGE == -11
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that says it is on another device than those beside it."""
+    def get_device(self):
+        return 5
+
+
+def test_the_binding_refuses_workspaces_and_stats_of_another_device_or_size(monkeypatch):
+    """(With CPU tensors taken for ones of the current device, and the library's entry points for a list of what reached them.)"""
+    reached = []
+    monkeypatch.setattr(binding, "_on", lambda t: t.get_device())
+    monkeypatch.setattr(binding, "_call", lambda name, *args: reached.append(name))
+    monkeypatch.setattr(binding, "_stream", lambda stream: 0)
+    p = params(dtype=torch.float32, head_dim=64)
+    Q, K, lse, ws = torch.zeros(2, 8, 7, 64), torch.zeros(2, 4, 9, 64), torch.zeros(2, 8, 7), torch.zeros(4096, dtype=torch.uint8)
+    stats = kvm.new_stats("cpu")
+    cache = pages()
+    cache.of = (-1, 8, 64, torch.float32)
+    length = torch.zeros(8, dtype=torch.int32)
+    calls = {
+        "kvm_cross_attend": lambda ws, stats: kvm.kvm_cross_attend(p, Q, K, K, None, Q, lse, ws, stats=stats),
+        "kvm_shared_attend": lambda ws, stats: kvm.kvm_shared_attend(p, Q[:, :, 0].contiguous(), K[0], K[0], None, None, Q[:, :, 0].contiguous(), ws, stats=stats),
+        "kvm_paged_append": lambda ws, stats: kvm.kvm_paged_append(p, cache, None, None, None, K, K, None, length, stats=stats),
+    }
+    for name, call in calls.items():
+        call(ws, stats)
+        call(ws, None)
+        assert reached == [name, name]
+        for bad in (stats.as_subclass(Elsewhere), stats[:-1], torch.zeros(64, dtype=torch.uint8)[::2]):
+            with pytest.raises(ValueError):
+                call(ws, bad)
+        if name != "kvm_paged_append":
+            for bad in (ws.as_subclass(Elsewhere), ws[::2]):
+                with pytest.raises(ValueError):
+                    call(bad, None)
+            call(None, None)                          # (the library answers that: no workspace)
+            reached.pop()
+        assert reached == [name, name]
+        reached.clear()

@@ -206,7 +206,7 @@ int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, 
     if (n_new < 1 || n_new > KVM_MAX_ROWS) return KVM_E_SHAPE;
     if (rope_layout != KVM_ROPE_HALVES && rope_layout != KVM_ROPE_NEIGHBOURS) return KVM_E_PARAM;
     if (misaligned(k) || misaligned(v) || (q && (misaligned(q) || misaligned(q_out))) || (turns && misaligned(turns, 8)) ||
-        misaligned(len_out, 4) || (new_len && misaligned(new_len, 4)) || (pos && misaligned(pos, 4)))
+        misaligned(len_out, 4) || misaligned(stats, 4) || (new_len && misaligned(new_len, 4)) || (pos && misaligned(pos, 4)))
         return KVM_E_ALIGN;
     int64_t st[9];
     const int64_t vec = s.dtype == KVM_BF16 ? 8 : 4;
@@ -251,7 +251,7 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
     if (K_pre ? (pre_rows < 1 || pre_rows > KVM_MAX_ROWS) : pre_rows != 0) return KVM_E_SHAPE;
     if (own && (rc = derive(own, false, pg)) != KVM_OK) return rc;
     if (too_many(s, pre_rows, own ? &pg : nullptr)) return KVM_E_SHAPE;
-    if (misaligned(q) || misaligned(out) || (K_pre && (misaligned(K_pre) || misaligned(V_pre))) || (pre_len && misaligned(pre_len, 4)))
+    if (misaligned(q) || misaligned(out) || misaligned(stats, 4) || (K_pre && (misaligned(K_pre) || misaligned(V_pre))) || (pre_len && misaligned(pre_len, 4)))
         return KVM_E_ALIGN;
     const SharedWork w = plan_shared(s, pre_rows, own ? &pg : nullptr, ws);
     if (!ws || ws_bytes < w.bytes) return KVM_E_WORKSPACE;
@@ -299,7 +299,7 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
     const int rc = check_cross(p, n_q, rows, s);
     if (rc != KVM_OK) return rc;
     if (!Q || !K || !V || !O || !lse || !O_in != !lse_in) return KVM_E_NULL;
-    if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O) || misaligned(lse, 4) || (len && misaligned(len, 4)) ||
+    if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(O) || misaligned(lse, 4) || misaligned(stats, 4) || (len && misaligned(len, 4)) ||
         (O_in && (misaligned(O_in) || misaligned(lse_in, 4))))
         return KVM_E_ALIGN;
     const CrossWork w = plan_cross(s, n_q, rows, ws);

@@ -177,3 +177,14 @@ def test_the_binding_refuses_workspaces_and_stats_of_another_device_or_size(monk
             reached.pop()
         assert reached == [name, name]
         reached.clear()
+
+
+def test_misaligned_stats_are_refused(lib):
+    """(Without the check a kernel that reports something stores a word at such an address.)"""
+    p, c = params(), pages()
+    assert lib.kvm_paged_append(ctypes.byref(p), ctypes.byref(c), OK, ctypes.c_int32(1), vp(0), OK, OK, ctypes.c_int32(0), OK, OK, OK, None, OK,
+                                vp(4098), vp(0)) == ALIGN
+    assert lib.kvm_shared_attend(ctypes.byref(p), OK, OK, OK, ctypes.c_int32(10), vp(0), ctypes.byref(c), OK, vp(4098), vp(0), ctypes.c_size_t(0),
+                                 vp(0)) == ALIGN
+    assert lib.kvm_cross_attend(ctypes.byref(p), OK, ctypes.c_int32(3), OK, OK, ctypes.c_int32(10), vp(0), vp(0), vp(0), OK, OK, vp(4098), vp(0),
+                                ctypes.c_size_t(0), vp(0)) == ALIGN

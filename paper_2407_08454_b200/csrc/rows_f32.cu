@@ -212,11 +212,14 @@ template <typename T, int D> __global__ void __launch_bounds__(NT8) rows8_kernel
 // On warp-level matrix products: an fp32 number is the sum of three bf16 numbers (each rounded to the nearest, what is left after two is below
 // 2^-17 of it and after three below 2^-26), and of the nine products of two such sums the six that reach 2^-26 are kept:
 //   x y = x1 y1 + (x1 y2 + x2 y1) + (x1 y3 + x2 y2 + x3 y1),
-// accumulated in fp32, the small ones first.  A warp has 16 query rows, whose three planes stay in registers; the block's four warps share
+// accumulated in fp32: of the logits the five small ones apart from the large one, and of O each 16 keys by themselves, the small ones first, which
+// ordinary additions then join.  (The matrix unit does not round to the nearest: what is added to a long sum again and again loses on one side.
+// With one accumulator for all, 30,000 keys of values of one sign came out 3.4e-5 of themselves too small, so 4e-8.)
+// A warp has 16 query rows, whose three planes stay in registers; the block's four warps share
 // the planes of 32 keys and values, made while they are written to shared memory (16-byte pieces swizzled by the row, so that ldmatrix
 // meets no bank conflict).  The weights are split in registers: what a lane holds of the first product is what it needs for the second.
-// (By products on the fp32 pipes, 64 x 64 blocks: 28.7 TFLOP/s with 64 channels, 31.9 with 128; this 43.6 and 43.0, which is
-// 260 of bf16 products: 16 heads x 1024 queries x 2048 keys.)
+// (By products on the fp32 pipes, 64 x 64 blocks: 28.7 TFLOP/s with 64 channels, 31.9 with 128; this 42.0 and 44.8, which is
+// 250 to 270 of bf16 products: 16 heads x 1024 queries x 2048 keys.)
 constexpr int KEYS = 32;
 // Three planes of two numbers, packed in pairs.  (An infinite number's rest would be NaN: it is none.)
 __device__ __forceinline__ void split2(float x, float y, uint32_t (&p)[3]) {
@@ -299,11 +302,11 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
         __syncthreads();
         if (AHEAD && r + KEYS < r1) t.load(a.k, u, r + KEYS, r1);
         // ---- logits: 16 rows x 32 keys
-        float x[4][4];                                                   // keys 8 n + 2 tig, + 1 of rows gid (first two), gid + 8
+        float x[4][4], small[4][4];                                      // keys 8 n + 2 tig, + 1 of rows gid (first two), gid + 8
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[n][e] = 0.f;
+            for (int e = 0; e < 4; ++e) x[n][e] = small[n][e] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             uint32_t kf[3][2][4];                                        // plane, 16 keys: channels 0..7, 8..15 of the first 8, of the last 8
@@ -317,7 +320,7 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
 #pragma unroll
             for (int i = 0; i < 6; ++i)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) mma16816(x[n], q[ks][PA[i]], kf[PB[i]][n >> 1][(n & 1) * 2], kf[PB[i]][n >> 1][(n & 1) * 2 + 1]);
+                for (int n = 0; n < 4; ++n) mma16816(i < 5 ? small[n] : x[n], q[ks][PA[i]], kf[PB[i]][n >> 1][(n & 1) * 2], kf[PB[i]][n >> 1][(n & 1) * 2 + 1]);
         }
         // ---- weights
         float mn[2] = {m[0], m[1]};
@@ -325,7 +328,7 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (!slive[n * 8 + 2 * tig + (e & 1)]) x[n][e] = -INFINITY;
+                x[n][e] = slive[n * 8 + 2 * tig + (e & 1)] ? x[n][e] + small[n][e] : -INFINITY;
                 mn[e >> 1] = fmaxf(mn[e >> 1], x[n][e]);
             }
         float alpha[2];
@@ -368,10 +371,15 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
                     const int key = kt * 16 + (lane & 15), piece = j * 2 + (lane >> 4);
                     ldsm4_t(vf[pl], base + (3 + pl) * PLANE + key * (D * 2) + ((piece ^ (key & 7)) << 4));
                 }
+                float c[2][4] = {};
 #pragma unroll
                 for (int i = 0; i < 6; ++i)
 #pragma unroll
-                    for (int z = 0; z < 2; ++z) mma16816(o[2 * j + z], w[PA[i]], vf[PB[i]][z * 2], vf[PB[i]][z * 2 + 1]);
+                    for (int z = 0; z < 2; ++z) mma16816(c[z], w[PA[i]], vf[PB[i]][z * 2], vf[PB[i]][z * 2 + 1]);
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[2 * j + z][e] += c[z][e];
             }
         }
     }

@@ -181,3 +181,27 @@ def test_a_mark_of_what_gave_up_stays(B, Hq, Hkv, n_q, rows, D, dtype, in_place)
             ref = Rows(Q[0, h], K[0, h // G], V[0, h // G], 1.0 / math.sqrt(D)).joined(O_in[0, h], lse_in[0, h])
             close(O[0, h, 2:], ref.O[2:], ref.O_bound(dtype)[2:], h)
             close(lse[0, h, 2:], ref.lse[2:], ref.lse_bound()[2:], h)
+
+
+@pytest.mark.parametrize("n_q,D", [(512, 128), (768, 64)])
+def test_fp32_long_sums_do_not_lose_on_one_side(n_q, D):
+    """Many keys in one piece, values of one sign, logits near zero: errors of single additions have to cancel.
+    O is a sum of N = rows / 16 terms, rounded after each addition by at most 2^-24 of the running sum.  Rounded to the nearest, these errors
+    are independent and uniform: together a standard deviation of 2^-24 sqrt(N) / 3 of the whole; six of them are 2^-23 sqrt(N).
+    Beside that 2^-21 for the logits and their exponentials (all below 1), twice (numerator and denominator), 17 roundings of 2^-24 within a term's
+    products, the value's planes, the division and the store, 2^-24 each: below 2^-19.  (Losing half a step of 2^-24 at each of six products a term
+    instead would be 2^-25 * 6 N / 2 = 1.1e-4 here.)"""
+    H, rows = 37, 20000
+    g = torch.Generator().manual_seed(51)
+    p = kvm.make_params(1, H, H, 1, D, torch.float32)
+    assert kvm.kvm_cross_workspace_bytes(p, n_q, rows) <= 256
+    Q = 0.05 * torch.randn(1, H, n_q, D, generator=g)
+    K, V = (torch.randn(1, H, rows, D, generator=g) for _ in range(2))
+    V = V.abs() + 0.5
+    O, lse = torch.empty_like(Q, device="cuda"), torch.empty(1, H, n_q, device="cuda")
+    ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n_q, rows), dtype=torch.uint8, device="cuda")
+    kvm.kvm_cross_attend(p, Q.cuda(), K.cuda(), V.cuda(), None, O, lse, ws)
+    for h in (0, 17, 36):
+        ref = Rows(Q[0, h], K[0, h], V[0, h], 1.0 / math.sqrt(D))
+        close(O[0, h], ref.O, ref.O * (2.0 ** -19 + 2.0 ** -23 * math.sqrt(rows / 16)), h)
+        close(lse[0, h], ref.lse, ref.lse_bound(), h)

@@ -37,9 +37,9 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
     constexpr int N = Vec<T>::N, LPT = D / (2 * N), TPB = APPEND_NT / LPT;      // lanes per token, tokens per block
     const int lane = threadIdx.x % LPT;
     const long long tokens = (long long)a.B * a.T, x = (long long)blockIdx.x * TPB + threadIdx.x / LPT;
+    const unsigned warp_lanes = __ballot_sync(0xffffffffu, x < tokens);
     if (x >= tokens) return;                    // (leaving early counts as letting the next kernel lie ready)
     const int b = (int)(x / a.T), t = (int)(x % a.T);
-    const unsigned group = ((1u << LPT) - 1u) << (threadIdx.x % 32 / LPT * LPT);       // the token's lanes
     const int o0 = NEIGHBOURS ? lane * 2 * N : lane * N, o1 = NEIGHBOURS ? o0 + N : o0 + D / 2;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -106,7 +106,9 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
                     a.stats->status = KVM_E_PAGE;
                 }
             }
-            __syncwarp(group);                  // (the token's lanes have all read the length, which may be moved in place)
+            // (The token's lanes have all read the length, which may be moved in place.  The whole warp takes the same rounds: gathered at once, where
+            // each token's lanes by themselves take it apart, 8 x 2048 tokens 65.1 -> 68.2 us.)
+            __syncwarp(warp_lanes);
             if (a.len_out && t == 0 && lane == 0) a.len_out[u] = min(start[i] + cnt, a.c.room());
         }
     }

@@ -95,8 +95,9 @@ template <typename T, int D> struct RowTo {
     // (live: a row of the unit; of those past its last one nothing is read)
     __device__ __forceinline__ RowTo(const Args& args, int u, int item, int piece, int row, int m_row, bool live, float m0, float l0)
         : a(args), state(args.pieces > 1 || args.st.o),
-          at(state ? (((size_t)u * args.st.items + item) * args.pieces + piece) * args.st.rows + row : (size_t)args.q.at(u, m_row)), m(m0), l(l0),
-          end(m0, l0, l0, live && !state ? args.out.lse_in : nullptr, at) {}
+          at(state ? (((size_t)u * args.st.items + item) * args.pieces + piece) * args.st.rows + row : (size_t)args.q.at(u, m_row)), m(m0), l(l0) {
+        if (!state) end = RowEnd(m0, l0, l0, live ? args.out.lse_in : nullptr, at);
+    }
     // E neighbouring channels from channel c
     template <int E> __device__ __forceinline__ void channels(int c, const float* o) const {
 #pragma unroll

@@ -93,6 +93,7 @@ __device__ __forceinline__ float rescale2(float m, float M) { return m == -INFIN
 // (l = 0: no keys, the row is what is joined in, bit for bit.  NaN sums, and a NaN lse_in, are the mark of a wait that gave up, and stay.)
 struct RowEnd {
     float f, f_in, lse;
+    __device__ __forceinline__ RowEnd() {}
     __device__ __forceinline__ RowEnd(float m, float l, float lr, const float* lse_in, long long row) {
         const bool none = l == 0.f;
         f = none ? 0.f : 1.f / lr;

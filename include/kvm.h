@@ -380,7 +380,7 @@ int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, 
  *   out          [batch, n_q_heads, D] in p->dtype, written: softmax over the prefix's and the own rows together; zeros where there
  *                are none; NaN where a bounded wait inside the kernel gave up
  * bf16: fp32 accumulation and softmax, the weights enter the product with V rounded to bf16 and are divided by the sum of the
- * rounded ones.  fp32: fp32 arithmetic, or (more than 16 query rows per KV head) tensor cores on every number as the sum of three bf16
+ * rounded ones; logits (scale * q.k) beyond 2^27, which fp32 holds to no better than 8, may give NaN.  fp32: fp32 arithmetic, or (more than 16 query rows per KV head) tensor cores on every number as the sum of three bf16
  * ones, of whose products those below 2^-26 are left out; an infinite value among the rows may then give NaN where fp32 arithmetic gives
  * infinity.  At least one of K_pre and own is given.
  */

@@ -13,6 +13,8 @@
 // A unit's part of a share leaves its state, which another kernel joins (a unit that is whole may go to the output).  Where units are few or
 // short each has a block of its own instead, and no second kernel.
 // Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones.
+#include <float.h>
+
 #include <mutex>
 
 #include "serve.cuh"
@@ -30,7 +32,7 @@ template <int D> constexpr int stages() { return D == 128 ? 3 : 6; }      // 24 
 constexpr int RING_BYTES = 3 * 8192;
 constexpr int MIN_BLOCKS = 2;               // fewest blocks of a warp's share (bounds the number of parts)
 constexpr int KEPT = 1024;                  // items whose lengths are kept in shared memory
-constexpr float LOWEST = -1e30f, RESCALE_STEP = 8.f;
+constexpr float LOWEST = -FLT_MAX, RESCALE_STEP = 8.f;      // (LOWEST: the reference before the first row, which any logit outgrows)
 
 struct Args {
     const __nv_bfloat16* q;                 // [units, G, D]

@@ -14,6 +14,8 @@
 //     of the product (16 keys at a time; the last ones' rows of V are zeroed in shared memory).
 // Bound by the exponentials and the softmax around them where there are many rows (see prefill_tc.cu for the clocks), by bandwidth where
 // a unit has one tile (64 KB of keys and values per step of about 2,800 clocks at an SM's share).
+#include <float.h>
+
 #include <initializer_list>
 #include <mutex>
 #include <type_traits>
@@ -39,7 +41,7 @@ constexpr float RESCALE_STEP = 8.f;     // a row's reference moves when outgrown
 constexpr int P_FIRST = 96;             // keys of a step whose P is handed over first
 constexpr uint32_t S_COLS = TILE, O_COL0 = 2 * S_COLS;
 constexpr int NEAR = 64;
-constexpr float LOWEST = -1e30f;        // the reference before the first key (a row of -inf logits keeps it, and weighs nothing)
+constexpr float LOWEST = -FLT_MAX;      // the reference before the first key, which any logit outgrows (a row of -inf logits keeps it, and weighs nothing)
 
 struct __align__(8) Bars {
     uint64_t q_full[2], q_empty[2], k0_full, k0_done;   // an item's Q tiles; its first K tile, loaded and used
@@ -566,6 +568,10 @@ rows_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             o_ph ^= 1;
             tc_fence_after();
+            // Logits enter the exponent by one multiply-add, less a reference that is a rounded product.  From 2^27 on half a step of it is more than
+            // exponentials bear: all weights of the row may be 0 or one infinite.  Such a row says so.  (Products rounded first would do, by a branch
+            // in every step: 3 % of all calls' time.)
+            if (m != LOWEST && !(l > 0.f && l < INFINITY)) l = lr = NAN;
             // 128 bytes of the warp's 32 rows at a time through shared memory to the copy engine, which takes them out beside the next
             // piece (stored by the threads, 64 KB of two tiles hold the softmax up for 2,000 clocks more).
             // (In loops: unrolled, these instructions are fetched anew for every piece.)

@@ -205,3 +205,54 @@ def test_fp32_long_sums_do_not_lose_on_one_side(n_q, D):
         ref = Rows(Q[0, h], K[0, h], V[0, h], 1.0 / math.sqrt(D))
         close(O[0, h], ref.O, ref.O * (2.0 ** -19 + 2.0 ** -23 * math.sqrt(rows / 16)), h)
         close(lse[0, h], ref.lse, ref.lse_bound(), h)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,n_q,rows,D", [(1, 2, 1, 40, 300, 64), (1, 4, 2, 150, 6000, 128), (1, 5, 5, 9, 24000, 64), (1, 2, 1, 3, 90, 128)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logits_far_below_zero(B, Hq, Hkv, n_q, rows, D, dtype):
+    """Logits of -1e31 and -2e31: numbers like others, of which the larger takes all the weight.  (On the tensor cores, whose multiply-adds bear
+    references up to 2^27, a row may be NaN instead, as documented, but nothing else.)"""
+    g = torch.Generator().manual_seed(61)
+    p = kvm.make_params(B, Hq, Hkv, 1, D, dtype, softmax_scale=0.125)
+    Q, K = torch.zeros(B, Hq, n_q, D), torch.zeros(B, Hkv, rows, D)
+    Q[..., 5], K[..., 5] = 1e16, -1.6e16
+    top = torch.randint(0, rows, (Hkv,), generator=g)
+    for h in range(Hkv):
+        K[0, h, top[h], 5] = -8e15
+    Q, K, V = Q.to(dtype), K.to(dtype), torch.randn(B, Hkv, rows, D, generator=g).to(dtype)
+    O, lse = torch.empty(B, Hq, n_q, D, dtype=dtype, device="cuda"), torch.empty(B, Hq, n_q, device="cuda")
+    ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n_q, rows), dtype=torch.uint8, device="cuda")
+    kvm.kvm_cross_attend(p, Q.cuda(), K.cuda(), V.cuda(), None, O, lse, ws)
+    for h in range(Hq):
+        u = h // (Hq // Hkv)
+        want = 0.125 * float(Q[0, h, 0, 5].double() * K[0, u, top[u], 5].double())
+        if dtype == torch.bfloat16:
+            gone = O[0, h].cpu().isnan().all(-1)
+            assert torch.equal(gone, lse[0, h].cpu().isnan()) and torch.equal(gone, O[0, h].cpu().isnan().any(-1))
+            O[0, h][gone.cuda()], lse[0, h][gone.cuda()] = V[0, u, top[u]].cuda(), want
+        # one weight of 1; an fp32 value is the sum of its three planes, off by 2^-26; the logit rounds a handful of times
+        assert bool(((O[0, h].cpu().double() - V[0, u, top[u]].double()).abs() <= 2.0 ** -24 * V[0, u, top[u]].double().abs()).all()), h
+        assert bool(((lse[0, h].cpu().double() - want).abs() <= 2.0 ** -20 * abs(want)).all()), h
+
+
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 20, 2.0 ** 25])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_logits_of_some_size(size, sign):
+    """bf16 on the tensor cores: logits around +-size, one ahead of the others by more than half its size."""
+    B, H, n_q, rows, D = 1, 2, 140, 700, 64
+    g = torch.Generator().manual_seed(63)
+    p = kvm.make_params(B, H, H, 1, D, torch.bfloat16, softmax_scale=0.5)
+    Q, K = torch.zeros(B, H, n_q, D), torch.zeros(B, H, rows, D)
+    Q[..., 7], K[..., 7] = 2.0 * size, sign if sign < 0 else 0.25
+    top = torch.randint(0, rows, (H,), generator=g)
+    for h in range(H):
+        K[0, h, top[h], 7] = -0.4375 if sign < 0 else 1.0
+    Q, K, V = Q.bfloat16(), K.bfloat16(), torch.randn(B, H, rows, D, generator=g).bfloat16()
+    O, lse = torch.empty(B, H, n_q, D, dtype=torch.bfloat16, device="cuda"), torch.empty(B, H, n_q, device="cuda")
+    ws = torch.empty(kvm.kvm_cross_workspace_bytes(p, n_q, rows), dtype=torch.uint8, device="cuda")
+    kvm.kvm_cross_attend(p, Q.cuda(), K.cuda(), V.cuda(), None, O, lse, ws)
+    for h in range(H):
+        want = size * (-0.4375 if sign < 0 else 1.0)
+        # (the reference may be off by half a step of the logit, by at most 2 here: the weight divides by itself)
+        assert torch.equal(O[0, h].cpu(), V[0, h, top[h]].expand(n_q, D)), h
+        assert bool(((lse[0, h].cpu().double() - want).abs() <= 2.0 ** -21 * abs(want)).all()), h

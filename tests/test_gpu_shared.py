@@ -205,3 +205,44 @@ def test_a_large_batch_of_which_a_part_is_empty(B, Hq, Hkv, D, prefix, held, R, 
 def test_more_units_than_keep_their_lengths(prefix):
     check(70, 16, 16, 64, prefix, 40, 16, torch.bfloat16)
     check(70, 32, 16, 128, prefix, 600, 32, torch.bfloat16, lengths=torch.randint(0, 4, (70, 16), generator=torch.Generator().manual_seed(6), dtype=torch.int32) ** 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,Hq,Hkv,D,prefix,held", [(2, 4, 2, 64, 0, 100), (2, 4, 2, 128, 0, 1500), (3, 4, 2, 128, 60, 40), (64, 40, 2, 128, 200, 33)])
+def test_logits_far_below_zero(B, Hq, Hkv, D, prefix, held, dtype):
+    """Logits of -1e31 and -2e31: numbers like others, of which the larger takes all the weight.  (Where the prefix has a kernel of its own, on the
+    tensor cores, a row may be NaN instead, as documented, but nothing else.)"""
+    g = torch.Generator().manual_seed(62)
+    G, R = Hq // Hkv, 16
+    p = kvm.make_params(B, Hq, Hkv, 1, D, dtype, softmax_scale=0.125)
+    lengths = torch.full((B, Hkv), held, dtype=torch.int32)
+    K, V, table = make_cache(g, B, Hkv, D, R, lengths, dtype)
+    K[:] = 0.0
+    K[..., 5] = -1.6e16
+    q = torch.zeros(B, Hq, D)
+    q[..., 5] = 1e16
+    q = q.to(dtype)
+    Kp = Vp = None
+    if prefix:
+        Kp, Vp = torch.zeros(Hkv, prefix, D).to(dtype), torch.randn(Hkv, prefix, D, generator=g).to(dtype)
+        Kp[..., 5] = -1.6e16
+        Kp[0, prefix // 2, 5] = -8e15                      # head 0's is in the prefix, the others' among their own rows
+    want = torch.empty(B, Hq, D, dtype=torch.float64)
+    for b in range(B):
+        for h in range(Hkv):
+            if prefix and h == 0:
+                top = Vp[0, prefix // 2]
+            else:
+                r = int(torch.randint(0, held, (1,), generator=g))
+                page = int(table[b * Hkv + h, r // R])
+                K[page, r % R, 5] = -8e15
+                top = V[page, r % R]
+            want[b, h * G:(h + 1) * G] = top.double()
+    own = kvm.make_pages(K.cuda(), V.cuda(), table.cuda(), lengths.cuda())
+    out = torch.empty(B, Hq, D, dtype=dtype, device="cuda")
+    ws = torch.empty(kvm.kvm_shared_workspace_bytes(p, prefix, own), dtype=torch.uint8, device="cuda")
+    kvm.kvm_shared_attend(p, q.cuda(), None if Kp is None else Kp.cuda(), None if Kp is None else Vp.cuda(), None, own, out, ws)
+    got = out.cpu().double()
+    if dtype == torch.bfloat16 and B > 8:
+        got = torch.where(got.isnan().all(-1, keepdim=True), want, got)
+    assert bool(((got - want).abs() <= 2.0 ** -24 * want.abs()).all())                     # (fp32: three planes, off by 2^-26)

@@ -299,3 +299,66 @@ def test_workspaces_and_stats_on_the_host_are_refused():
             kvm.kvm_shared_attend(p, q[:, :, 0].contiguous(), K[0], K[0], None, None, q[:, :, 0].contiguous(), w, stats=stats)
     with pytest.raises(kvm.KvmError):
         kvm.kvm_cross_attend(p, q, K, K, None, q.clone(), lse, None)
+
+
+def test_a_large_batch_decodes_beside_its_prefix():
+    """Append and shared attention step by step where the prefix has a kernel of its own: the paged kernel beside it reads lengths, queries and rows that the
+    call before has just written.  Some sequences begin without rows.  Called one after the other, and captured and replayed."""
+    g = torch.Generator().manual_seed(33)
+    B, Hq, Hkv, D, P, R, steps = 64, 8, 2, 128, 1200, 16, 4
+    G, U, room = Hq // Hkv, B * Hkv, 4
+    p = kvm.make_params(B, Hq, Hkv, 1, D, torch.bfloat16)
+    start = torch.randint(0, 30, (B, Hkv), generator=g, dtype=torch.int32)
+    start[::5] = 0
+    table = torch.randperm(U * room, generator=g).to(torch.int32).view(U, room)
+    first = [torch.randn(U * room, R, D, generator=g).bfloat16() for _ in range(2)]
+    pool, length = [x.cuda() for x in first], start.cuda()
+    cache = kvm.make_pages(pool[0], pool[1], table.cuda(), length)
+    q, k, v = (torch.randn(steps, B, h, 1, D, generator=g).bfloat16().cuda() for h in (Hq, Hkv, Hkv))
+    Kp, Vp = (torch.randn(Hkv, P, D, generator=g).bfloat16() for _ in range(2))
+    Kd, Vd, n_pre = Kp.cuda(), Vp.cuda(), torch.tensor([P, 900], dtype=torch.int32, device="cuda")
+    tr, pos = kvm.rope_turns(D), torch.full((B,), P, dtype=torch.int32, device="cuda")
+    q_rot, outs = torch.empty(steps, B, Hq, 1, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(steps, B, Hq, D, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((kvm.kvm_shared_workspace_bytes(p, P, cache),), 255, dtype=torch.uint8, device="cuda")
+
+    def run():
+        for s in range(steps):
+            kvm.kvm_paged_append(p, cache, pos, tr, q[s], k[s], v[s], q_rot[s], length)
+            kvm.kvm_shared_attend(p, q_rot[s].view(B, Hq, D), Kd, Vd, n_pre, cache, outs[s], ws)
+            pos.add_(1)
+
+    def reset():
+        for x, y in zip(pool, first):
+            x.copy_(y)
+        length.copy_(start)
+        pos.fill_(P)
+        outs.zero_()
+
+    torch.cuda.synchronize()
+    run()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in (outs, q_rot, length, *pool)]
+    Kc, Vc, qc = pool[0].cpu(), pool[1].cpu(), q_rot.cpu()
+    assert torch.equal(length.cpu(), start + steps)
+    for s in range(steps):
+        for b in (0, 5, 13, 31, 50, 63):
+            for h in range(Hkv):
+                rows = torch.arange(int(start[b, h]) + s + 1)
+                page = table[b * Hkv + h][rows // R].long()
+                m = (P, 900)[h]
+                ref = Rows(qc[s, b, h * G:(h + 1) * G, 0], torch.cat([Kp[h, :m], Kc[page, rows % R]]), torch.cat([Vp[h, :m], Vc[page, rows % R]]),
+                           1.0 / math.sqrt(D))
+                close(outs[s, b, h * G:(h + 1) * G], ref.O, ref.O_bound(torch.bfloat16), (s, b, h))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for _ in range(5):
+        reset()
+        graph.replay()
+        for x, w in zip((outs, q_rot, length, *pool), want):
+            assert torch.equal(x, w)
+    for _ in range(5):
+        reset()
+        run()
+        for x, w in zip((outs, q_rot, length, *pool), want):
+            assert torch.equal(x, w)

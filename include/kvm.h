@@ -362,7 +362,7 @@ int kvm_rope_turns(int32_t head_dim, double base, uint64_t* turns);
  *            q itself where q is contiguous, and may not overlap the inputs otherwise
  *   c        the cache: row len[u] + t of unit u receives the rotated key and the value; other rows are left as they are
  *   len_out  device [U] i32, written: the new lengths (at most max_pages * page_rows); c->len itself, or apart from it
- * fp32 arithmetic, one rounding at the store; angles are exact to 2^-25 of a turn.  stats: NULL or a device kvm_stats.
+ * fp32 arithmetic, one rounding at the store; angles are exact to 2^-31 of a turn.  stats: NULL or a device kvm_stats.
  */
 int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, int32_t n_new, const int32_t* new_len,
                      const int32_t* pos, const uint64_t* turns, int32_t rope_layout, const void* q, const void* k,

@@ -6,8 +6,8 @@
 // page, row).  A group of D / 2N lanes (N: elements of 16 bytes) owns a token: it computes the token's cosines and sines once and takes
 // the token's heads one after the other, ROUND at a time so that their loads leave together.  The angle is an integer product:
 // with the frequency as a 64-bit binary fraction of a turn the product with the position wraps around at whole turns, and
-// what is left, rounded to 24 bits, is the argument of sincospi: nothing is lost for far positions, and no 64-bit floating-point
-// arithmetic (2 results a clock and SM here) is needed.
+// what is left, rounded to 24 bits, is the argument of sincospi, and eight bits more turn its results by their first order: nothing is lost
+// for far positions, and no 64-bit floating-point arithmetic (2 results a clock and SM here) is needed.
 #include "serve.cuh"
 
 namespace kvm {
@@ -50,7 +50,12 @@ __global__ void __launch_bounds__(APPEND_NT) append_kernel(const AppendArgs a) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const uint64_t turn = p * __ldg(reinterpret_cast<const unsigned long long*>(a.turns) + lane * N + e);
-            sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, sn + e, cs + e);      // half turns: 2^-31
+            const int32_t a32 = (int32_t)(turn >> 32);                                            // half turns: 2^-31
+            const float a24 = (float)a32, rest = (float)(a32 - __float2int_rn(a24)) * 1.4629180792671596e-9f;      // (pi 2^-31)
+            float c, d;
+            sincospif(a24 * 4.656612873077393e-10f, &d, &c);
+            cs[e] = fmaf(-d, rest, c);
+            sn[e] = fmaf(c, rest, d);
         }
     }
     auto rotate = [&](uint4& r0, uint4& r1) {

@@ -207,3 +207,22 @@ def test_decode_steps_of_a_large_batch_with_lengths_in_place(B, Hq, Hkv, D, dtyp
         want[0][page, rows % R], want[1][page, rows % R] = k.view(U, D), v.view(U, D)
         assert torch.equal(length, start + s + 1)
     assert torch.equal(pool[0], want[0]) and torch.equal(pool[1], want[1]) and torch.equal(q_out, q)
+
+
+def test_angles_have_more_than_24_bits():
+    """fp32 pairs (1, 0), which come out as the cosine and the sine themselves.  sincospi is off by at most one unit in the last place, 2^-24 below 1; the
+    angle's last bits are added by one multiply-add, 2^-25; what is left of the angle is below 2^-31 half turns, 2^-29.3: together below 1.6 x 2^-24."""
+    B, H, D, T = 16, 2, 128, 64
+    g = torch.Generator().manual_seed(71)
+    pos = torch.randint(0, 1 << 20, (B,), generator=g, dtype=torch.int32)
+    q = torch.zeros(B, H, T, D)
+    q[..., :D // 2] = 1.0
+    lengths = torch.zeros(B, H, dtype=torch.int32)
+    K, V, table = make_cache(g, B, H, D, 16, lengths, torch.float32, room=T)
+    p = kvm.make_params(B, H, H, 1, D, torch.float32)
+    q_out, ln = torch.empty(B, H, T, D, device="cuda"), lengths.cuda()
+    kvm.kvm_paged_append(p, kvm.make_pages(K.cuda(), V.cuda(), table.cuda(), ln), pos.cuda(), kvm.rope_turns(D), q.cuda(), q.cuda(), q.cuda(), q_out, ln)
+    where = pos[:, None, None].to(F64) + torch.arange(T, dtype=F64)
+    # (the reference's own angle: 2^-53 of up to 2^20 / 2 pi turns, 2^-35)
+    want = rotate(q.to(F64), where.expand(B, H, T), turns(D), False)
+    within(q_out, want, torch.full_like(want, 1.6 * 2.0 ** -24 + 2.0 ** -32))

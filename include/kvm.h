@@ -377,12 +377,13 @@ int kvm_paged_append(const kvm_params* p, const kvm_pages* c, int32_t* len_out, 
  *   pre_len      NULL (every KV head holds pre_rows rows) or device [n_kv_heads] i32 (clamped to 0..pre_rows)
  *   own          NULL (no rows beside the prefix), or the paged cache of the sequences' own rows; not written.  batch * n_q_heads *
  *                (max_pages * page_rows + pre_rows) / 16 must stay below 2^31 (KVM_E_SHAPE)
- *   out          [batch, n_q_heads, D] in p->dtype, written: softmax over the prefix's and the own rows together; zeros where there
+ *   out          [batch, n_q_heads, D] in p->dtype, written, apart from the inputs: softmax over the prefix's and the own rows together; zeros where there
  *                are none; NaN where a bounded wait inside the kernel gave up
  * bf16: fp32 accumulation and softmax, the weights enter the product with V rounded to bf16 and are divided by the sum of the
- * rounded ones; logits (scale * q.k) beyond 2^27, which fp32 holds to no better than 8, may give NaN.  fp32: fp32 arithmetic, or (more than 16 query rows per KV head) tensor cores on every number as the sum of three bf16
- * ones, of whose products those below 2^-26 are left out; an infinite value among the rows may then give NaN where fp32 arithmetic gives
- * infinity.  At least one of K_pre and own is given.
+ * rounded ones; logits (scale * q.k) beyond 2^27, which fp32 holds to no better than 8, may give NaN.  fp32: fp32 arithmetic, or (more
+ * than 16 query rows per KV head) tensor cores on every number as the sum of three bf16 ones, of whose products those below 2^-26 are left
+ * out; a value among the rows that is infinite, or that bf16 rounds to infinity, may then give NaN or infinity where fp32 arithmetic gives
+ * a number or infinity.  At least one of K_pre and own is given.
  */
 int kvm_shared_workspace_bytes(const kvm_params* p, int32_t pre_rows, const kvm_pages* own, size_t* bytes);   /* Host only; pre_rows 0: no prefix. */
 int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, const void* V_pre, int32_t pre_rows,
@@ -398,8 +399,9 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
  *        lse_in [batch, n_q_heads, n_q] fp32, natural log: the result is then that over both sets of keys.  The next chunk of a
  *        prompt attends to its compressed past and to itself by kvm_prefill_attend, whose O and lse go in here.  Both or neither;
  *        they may be O and lse themselves, and may not overlap them otherwise
- *   O    [batch, n_q_heads, n_q, D] in p->dtype, written; a unit with no rows gives zeros (or O_in)
- *   lse  [batch, n_q_heads, n_q] fp32, written: ln of the sum over the keys of exp(scale * q.k); -inf without keys (or lse_in)
+ *   O    [batch, n_q_heads, n_q, D] in p->dtype, written, apart from Q, K, V; a unit with no rows gives zeros (or O_in)
+ *   lse  [batch, n_q_heads, n_q] fp32, written: ln of the sum over the keys of exp(scale * q.k); -inf without keys (or lse_in).
+ *        NaN in lse_in, the mark of a wait that gave up, stays NaN in O and lse; a unit with no rows passes O_in and lse_in on
  * Numerics as kvm_shared_attend.  bf16: a bounded wait that gave up leaves NaN and kvm_stats.status = KVM_E_DEVICE_TIMEOUT.
  */
 int kvm_cross_workspace_bytes(const kvm_params* p, int32_t n_q, int32_t rows, size_t* bytes);   /* Host only. */

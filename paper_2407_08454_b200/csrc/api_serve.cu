@@ -58,7 +58,7 @@ struct Carver {
 };
 
 // States of a fixed number of pieces per item (plan.mt rows each).
-States simt_states(const SimtPlan& plan, int units, int D, Carver& c) {
+States f32_states(const F32Plan& plan, int units, int D, Carver& c) {
     States s = {};
     const size_t slots = (size_t)units * plan.items * plan.pieces;
     s.rows = s.tile = plan.mt;
@@ -106,7 +106,7 @@ struct SharedWork {
     bool pre, own, fold;                        // fold: the prefix's rows go with each sequence's own
     TcPlan pre_tc;
     PagedPlan own_paged;
-    SimtPlan pre_plan, own_plan;
+    F32Plan pre_plan, own_plan;
     States pre_states, own_states;
     size_t bytes;
 };
@@ -132,15 +132,15 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
         w.pre_tc = tc_plan(s.Hkv, s.G, s.B, pre_rows, false);
         w.pre_states = tc_states(w.pre_tc, s.Hkv, s.D, s.G, c);
     } else if (w.pre) {
-        w.pre_plan = simt_plan(s.Hkv, s.B * s.G, pre_rows, s.D);
-        if (w.own || w.pre_plan.pieces > 1) w.pre_states = simt_states(w.pre_plan, s.Hkv, s.D, c);
+        w.pre_plan = f32_plan(s.Hkv, s.B * s.G, pre_rows, s.D);
+        if (w.own || w.pre_plan.pieces > 1) w.pre_states = f32_states(w.pre_plan, s.Hkv, s.D, c);
     }
     if (w.own && s.dtype == KVM_BF16) {
         w.own_paged = paged_plan(s, own->room(), w.pre);
         w.own_states = paged_states(w.own_paged, s.D, c);
     } else if (w.own) {
-        w.own_plan = simt_plan(s.U, s.G, own->room(), s.D);
-        if (w.pre || w.own_plan.pieces > 1) w.own_states = simt_states(w.own_plan, s.U, s.D, c);
+        w.own_plan = f32_plan(s.U, s.G, own->room(), s.D);
+        if (w.pre || w.own_plan.pieces > 1) w.own_states = f32_states(w.own_plan, s.U, s.D, c);
     }
     w.bytes = c.off + 256;
     return w;
@@ -148,7 +148,7 @@ SharedWork plan_shared(const Shape& s, int pre_rows, const Pages* own, void* ws)
 
 struct CrossWork {
     TcPlan tc;
-    SimtPlan plan;
+    F32Plan plan;
     States states;
     size_t bytes;
 };
@@ -161,8 +161,8 @@ CrossWork plan_cross(const Shape& s, int n_q, int rows, void* ws) {
         w.bytes = c.off + 256;
         return w;
     }
-    w.plan = simt_plan(s.U, s.G * n_q, rows, s.D);
-    if (w.plan.pieces > 1) w.states = simt_states(w.plan, s.U, s.D, c);
+    w.plan = f32_plan(s.U, s.G * n_q, rows, s.D);
+    if (w.plan.pieces > 1) w.states = f32_states(w.plan, s.U, s.D, c);
     w.bytes = c.off + 256;
     return w;
 }
@@ -272,8 +272,8 @@ int kvm_shared_attend(const kvm_params* p, const void* q, const void* K_pre, con
         if (w.pre && launch_rows_tc(s, w.pre_tc, s.Hkv, pre_q, pre_k, mine, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
         if (w.own && launch_rows_paged(s, w.own_paged, q, own_k, Fold{}, pre, w.own_states, w.pre ? nullptr : out, stats, st) != cudaSuccess) return KVM_E_CUDA;
     } else {
-        if (w.pre && launch_rows_simt(s, w.pre_plan, s.Hkv, pre_q, pre_k, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
-        if (w.own && launch_rows_simt(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.pre && launch_rows_f32(s, w.pre_plan, s.Hkv, pre_q, pre_k, w.pre_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+        if (w.own && launch_rows_f32(s, w.own_plan, s.U, own_q, own_k, w.own_states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     }
     if ((!w.pre_states.o && !w.own_states.o) || w.own_paged.alone) return KVM_OK;
     const int about = s.dtype == KVM_BF16 ? (w.own ? w.own_paged.grid * 4 / w.own_paged.items : 0) + (w.pre ? w.pre_tc.grid / (s.Hkv * w.pre_tc.items) : 0)
@@ -315,7 +315,7 @@ int kvm_cross_attend(const kvm_params* p, const void* Q, int32_t n_q, const void
         if (w.tc.whole) return KVM_OK;
         return launch_join_items(s, s.U, m, w.states, len, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
     }
-    if (launch_rows_simt(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
+    if (launch_rows_f32(s, w.plan, s.U, qs, ks, w.states, o, stats, st) != cudaSuccess) return KVM_E_CUDA;
     if (!w.states.o) return KVM_OK;
     return launch_join(s, s.U, m, &w.states, nullptr, nullptr, 0, w.plan.pieces, o, st) == cudaSuccess ? KVM_OK : KVM_E_CUDA;
 }

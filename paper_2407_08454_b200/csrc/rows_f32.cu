@@ -1,4 +1,4 @@
-// Attention of a unit's query rows over its keys in fp32 arithmetic, without a mask but the unit's length:
+// Attention of a unit's query rows over its keys for fp32 tensors, without a mask but the unit's length:
 //   o = softmax(c q K^T) V,  lse = ln sum exp(c q.k)
 // with one pass over the keys, a running maximum and sum per row, and, where there are few rows, the keys cut into pieces whose
 // states are joined by another kernel.
@@ -399,7 +399,7 @@ template <int D> __global__ void __launch_bounds__(NT64, D == 128 ? 2 : 3) rows6
     }
 }
 
-template <int D> cudaError_t launch_t(const Args& a, const SimtPlan& plan, int units, cudaStream_t st) {
+template <int D> cudaError_t launch_t(const Args& a, const F32Plan& plan, int units, cudaStream_t st) {
     const dim3 grid(plan.items, plan.pieces, units);
     if (plan.mt == 8) return launch_dependent(rows8_kernel<float, D>, grid, dim3(NT8), 0, st, a);
     constexpr size_t smem = 6 * KEYS * D * 2;                            // (48 KB of planes and what is static: an opt-in)
@@ -424,8 +424,8 @@ template <int D> cudaError_t launch_t(const Args& a, const SimtPlan& plan, int u
 // Pieces: the number whose blocks fill the SMs best in whole rounds of what is at work at the same time (five blocks of 8 rows to an SM; of
 // 64 rows two with 128 channels, three with 64), a few per cent given away for each more, but none with less than 128 keys where all are
 // there.  (56 units x 160 rows x 3542 keys x 128: 168 blocks in one piece each, 1.8 times what whole rounds take.)
-SimtPlan simt_plan(int units, int m, int rows, int D) {
-    SimtPlan p;
+F32Plan f32_plan(int units, int m, int rows, int D) {
+    F32Plan p;
     p.mt = m <= 16 ? 8 : 64;
     p.items = (m + p.mt - 1) / p.mt;
     const long long blocks = (long long)units * p.items, room = SMS * (p.mt == 8 ? 5 : D == 128 ? 2 : 3);
@@ -439,7 +439,7 @@ SimtPlan simt_plan(int units, int m, int rows, int D) {
     return p;
 }
 
-cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
+cudaError_t launch_rows_f32(const Shape& s, const F32Plan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                              kvm_stats* stats, cudaStream_t st) {
     if (units > 65535 || plan.pieces > 65535) return cudaErrorInvalidValue;
     const Args a = {q, k, states, out, stats, s.scale * LOG2E, plan.pieces};

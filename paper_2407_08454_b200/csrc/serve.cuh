@@ -136,7 +136,7 @@ struct Beside {
 };
 // SMs for the prefix, such that both parts end at about the same time (by all lanes of a warp).  Measured side by side, us: the prefix 14
 // and 2.4 for each of a CTA's steps (128 keys, up to 256 query rows); the own rows 8 and 0.137 for 16 rows of 128 channels on one SM
-// (60 GB/s).  64 sequences of 768 rows over 16384 x 8 heads, own rows on 60 / 70 / 80 / 90 SMs: 71.5 / 64.4 / 61.1 / 67.2 us, one after the other 80;
+// (60 GB/s).  (Taken with 128 channels and two query tiles; a step of one tile, or of 64 channels, is shorter.)  64 sequences of 768 rows over 16384 x 8 heads, own rows on 60 / 70 / 80 / 90 SMs: 71.5 / 64.4 / 61.1 / 67.2 us, one after the other 80;
 // 16 x 32 of 292 rows over 2048 x 32 heads, on 48 / 60 / 70 / 80 / 90: 39.4 / 34.4 / 35.0 / 36.4 / 39.9, one after the other 43.
 constexpr int OWN_MOST = 128;
 __device__ __forceinline__ int prefix_sms(long long steps, long long blocks, int D) {
@@ -173,13 +173,13 @@ cudaError_t launch_append(const Shape& s, const Pages& c, int32_t* len_out, int 
                           const uint64_t* turns, int neighbours, const void* q, const void* k, const void* v, const int64_t* strides,
                           void* q_out, kvm_stats* stats, cudaStream_t st);
 
-// Attention of all query rows over all keys of their units in fp32 arithmetic, for fp32 tensors.  With one piece per item the
-// result goes to `out`, else the states to `states`.
-struct SimtPlan {
+// Attention of all query rows over all keys of their units, for fp32 tensors: on the fp32 pipes (mt = 8) or on matrix products of three bf16
+// planes (mt = 64), see rows_f32.cu.  With one piece per item the result goes to `out`, else the states to `states`.
+struct F32Plan {
     int mt, items, pieces;                      // query rows of an item, items of a unit, pieces of an item
 };
-SimtPlan simt_plan(int units, int m, int rows, int D);
-cudaError_t launch_rows_simt(const Shape& s, const SimtPlan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
+F32Plan f32_plan(int units, int m, int rows, int D);
+cudaError_t launch_rows_f32(const Shape& s, const F32Plan& plan, int units, const Queries& q, const Keys& k, const States& states, const Output& out,
                              kvm_stats* stats, cudaStream_t st);
 
 // The same on the tensor cores (bf16, contiguous keys): equal shares of all items' steps per CTA, see rows_tc.cu.

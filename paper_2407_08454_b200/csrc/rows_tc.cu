@@ -12,8 +12,8 @@
 //     tiles, so that one's exponentials run under the other's products here too; their states are joined like those of pieces.
 //   - The last key tile is cut where the unit ends: logits beyond are -inf, and what V holds there, which may be anything, is kept out
 //     of the product (16 keys at a time; the last ones' rows of V are zeroed in shared memory).
-// Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones: their rest as a second product would take a pair's
-// step from 2,048 clocks of products to 3,072, more than it takes now.
+// Weights are rounded to bf16 for the second product and divided by the sum of the rounded ones: their rest as a second product would add half
+// as many clocks again to the 2,048 that a pair's step has of products.
 // Bound by the exponentials and the softmax around them where there are many rows (see prefill_tc.cu for the clocks), by bandwidth where
 // a unit has one tile (64 KB of keys and values per step of about 2,800 clocks at an SM's share).
 #include <float.h>
